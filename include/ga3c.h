@@ -420,6 +420,115 @@ int ga3c_predict_static(int n_actions, int math, const float *theta_dev, const u
 /* Shape and capacities the context was created with (any pointer may be NULL). */
 int ga3c_get_desc(const ga3c_ctx *ctx, ga3c_net_desc *desc, int *max_predict_batch, int *max_train_frames);
 
+/* ---- memory of an agent ------------------------------------------------------
+ *
+ * The network above sees the few frames of its input.  Two operators give an
+ * agent a memory: attention with a decay for each head, whose state a
+ * prediction advances by one step and an update runs over whole segments, and
+ * group norm with an activation for what is read out of it.  They work on the
+ * caller's tensors and keep nothing between calls.
+ *
+ * Tensors of queries, keys, values and their gradients hold elements of one
+ * type (dtype) in device memory: element (token, head, i) lies at
+ * data[token * token_stride + head * head_stride + i], strides in elements, so
+ * that they may be slices of one matrix.  Strides are not negative; rows of an
+ * output do not overlap each other, nor any input. */
+#define GA3C_F32  0
+#define GA3C_BF16 1
+#define GA3C_MAX_HEADS 128
+#define GA3C_MAX_HEAD_DIM 128
+
+typedef struct {
+    void *data;
+    int64_t token_stride, head_stride;
+} ga3c_heads;
+
+/*   decay   host array [n_heads], each in [0, 1]; read at call time
+ *   scale   multiplies what is read out */
+typedef struct {
+    int n_heads, key_dim, value_dim;      /* 1 .. GA3C_MAX_HEADS, 1 .. GA3C_MAX_HEAD_DIM */
+    int dtype;                            /* GA3C_F32 or GA3C_BF16; states are fp32 with either */
+    const float *decay;
+    float scale;
+} ga3c_decay_desc;
+
+/* Attention with a decay for each head over n_segments sequences laid end to
+ * end.  In each head, from the first token of a segment on, with the state S
+ * [value_dim][key_dim] that state_in gives (zero without it):
+ *   S = 0 where starts[t] != 0;  S = decay S + v_t k_t^T;  out_t = scale S q_t
+ * and state_out receives S behind the segment's last token.
+ *   q, k          [n_tokens][n_heads][key_dim];  v, out [n_tokens][n_heads][value_dim]
+ *   seg_start_dev i32 [n_segments+1] as for ga3c_train_step_ragged (checked no
+ *                 more than there: a bad table gives wrong results, no access
+ *                 outside the arrays), or NULL: segments of equal length
+ *   starts_dev    u8 [n_tokens], non-zero = an episode begins with this token,
+ *                 whatever the segment; or NULL
+ *   state_in_dev, state_out_dev  f32 [n_segments][n_heads][value_dim][key_dim],
+ *                 each may be NULL; a segment without tokens hands its state on
+ *   workspace_dev scratch of at least ga3c_decay_attention_workspace() bytes,
+ *                 16-byte aligned, contents irrelevant before and after; calls
+ *                 that may overlap need one each
+ * Products of fp32 tensors and all states are fp32 sums; with bfloat16 tensors
+ * an output is within a few roundings to bfloat16 of the exact one. */
+int ga3c_decay_attention(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
+                         const ga3c_heads *out, const int32_t *seg_start_dev, const uint8_t *starts_dev, int n_segments,
+                         int n_tokens, const float *state_in_dev, float *state_out_dev, void *workspace_dev,
+                         size_t workspace_bytes, void *stream);
+
+/* Its gradient: from dout (like out) and dstate_out_dev (like state_out, may be
+ * NULL = 0) to dq, dk, dv (like q, k, v) and dstate_in_dev (may be NULL).  The
+ * decays are constants.  state_in_dev is the one the forward call was given. */
+int ga3c_decay_attention_grad(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
+                              const ga3c_heads *dout, const ga3c_heads *dq, const ga3c_heads *dk, const ga3c_heads *dv,
+                              const int32_t *seg_start_dev, const uint8_t *starts_dev, int n_segments, int n_tokens,
+                              const float *state_in_dev, const float *dstate_out_dev, float *dstate_in_dev,
+                              void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Scratch for either call, in bytes (0 for a bad description). */
+size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *desc, int n_segments, int n_tokens);
+
+/* One token of each of n agents, whose states lie in states_dev f32
+ * [n_slots][n_heads][value_dim][key_dim] and are advanced in place.
+ *   slots_dev   i32 [n], the state of each token, or NULL: token i has state i
+ *               (n <= n_slots then).  A slot outside [0, n_slots) is a padded
+ *               entry: a state of zeros that is not kept.  Tokens that name the
+ *               same slot are consecutive steps of it, in the order of the array.
+ *   starts_dev  u8 [n] as above, or NULL
+ * Tokens and states are as for ga3c_decay_attention on segments of one token. */
+int ga3c_decay_attention_step(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
+                              const ga3c_heads *out, const int32_t *slots_dev, const uint8_t *starts_dev, int n,
+                              float *states_dev, int n_slots, void *stream);
+
+/* Group norm with an activation.  A sample is n_positions rows of `channels`
+ * elements (a map with its channels last, or one token); a group is
+ * channels / groups neighbouring channels of all its positions:
+ *   y = act((x - mean) * rstd * gamma + beta),  rstd = 1 / sqrt(var + eps)
+ * with mean and (biased) variance over the sample's group, gamma and beta f32
+ * [channels].  Position i of x starts at x + i * x_stride elements, i counting
+ * through all samples; x_stride, y_stride >= channels.
+ *   stats_dev   f32 [n_samples][groups][2] receives mean and rstd, which the
+ *               gradient needs; may be NULL
+ *   workspace_dev  as above, of ga3c_group_norm_workspace() bytes
+ * The gradient gives dx (like x) from dy (like y), and dgamma, dbeta f32
+ * [channels] summed over all samples and positions in a fixed order. */
+#define GA3C_ACT_NONE 0
+#define GA3C_ACT_RELU 1
+#define GA3C_ACT_SILU 2                   /* z / (1 + exp(-z)) */
+typedef struct {
+    int channels, groups;
+    int dtype, act;
+    float eps;
+} ga3c_norm_desc;
+
+int ga3c_group_norm(const ga3c_norm_desc *desc, const void *x_dev, int64_t x_stride, const float *gamma_dev,
+                    const float *beta_dev, void *y_dev, int64_t y_stride, float *stats_dev, int n_samples, int n_positions,
+                    void *workspace_dev, size_t workspace_bytes, void *stream);
+int ga3c_group_norm_grad(const ga3c_norm_desc *desc, const void *x_dev, int64_t x_stride, const void *dy_dev,
+                         int64_t dy_stride, const float *gamma_dev, const float *beta_dev, const float *stats_dev,
+                         void *dx_dev, int64_t dx_stride, float *dgamma_dev, float *dbeta_dev, int n_samples,
+                         int n_positions, void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t ga3c_group_norm_workspace(const ga3c_norm_desc *desc, int n_samples, int n_positions);
+
 /* Thread-local text of the last error on this thread ("" if none). */
 const char *ga3c_last_error(void);
 

@@ -43,6 +43,19 @@ class _SchedConfig(C.Structure):
                 ("seed", C.c_uint64), ("hp", _HParams), ("adjust_margin", C.c_float)]
 
 
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _DecayDesc(C.Structure):
+    _fields_ = [("n_heads", C.c_int), ("key_dim", C.c_int), ("value_dim", C.c_int), ("dtype", C.c_int),
+                ("decay", C.POINTER(C.c_float)), ("scale", C.c_float)]
+
+
+class _NormDesc(C.Structure):
+    _fields_ = [("channels", C.c_int), ("groups", C.c_int), ("dtype", C.c_int), ("act", C.c_int), ("eps", C.c_float)]
+
+
 class Prediction(C.Structure):
     _fields_ = [("agent", C.c_int32), ("action", C.c_int32), ("value", C.c_float), ("policy_version", C.c_int32)]
 
@@ -124,7 +137,9 @@ EXPORTS = ("ga3c_create", "ga3c_destroy", "ga3c_params_count", "ga3c_params_offs
            "ga3c_sched_submit_predict_many", "ga3c_sched_submit_trajectory_many",
            "ga3c_sched_tick", "ga3c_sched_poll", "ga3c_sched_drain", "ga3c_sched_get_stats", "ga3c_sched_last_error",
            "ga3c_tuner_create", "ga3c_tuner_report", "ga3c_tuner_state", "ga3c_tuner_destroy", "ga3c_tuner_set_margin",
-           "ga3c_tuner_progress")
+           "ga3c_tuner_progress",
+           "ga3c_decay_attention", "ga3c_decay_attention_grad", "ga3c_decay_attention_step", "ga3c_decay_attention_workspace",
+           "ga3c_group_norm", "ga3c_group_norm_grad", "ga3c_group_norm_workspace")
 
 
 def load_library() -> C.CDLL:
@@ -175,6 +190,16 @@ def load_library() -> C.CDLL:
     lib.ga3c_tuner_set_margin.argtypes = [vp, C.c_double]
     lib.ga3c_tuner_progress.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
     lib.ga3c_use_generic_kernels.argtypes = [vp, i32]
+    heads, i64 = C.POINTER(_Heads), C.c_int64
+    lib.ga3c_decay_attention.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.ga3c_decay_attention_grad.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 7 + [vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.ga3c_decay_attention_step.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, vp, i32, vp]
+    lib.ga3c_decay_attention_workspace.argtypes = [C.POINTER(_DecayDesc), i32, i32]
+    lib.ga3c_decay_attention_workspace.restype = sz
+    lib.ga3c_group_norm.argtypes = [C.POINTER(_NormDesc), vp, i64, vp, vp, vp, i64, vp, i32, i32, vp, sz, vp]
+    lib.ga3c_group_norm_grad.argtypes = [C.POINTER(_NormDesc), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i32, i32, vp, sz, vp]
+    lib.ga3c_group_norm_workspace.argtypes = [C.POINTER(_NormDesc), i32, i32]
+    lib.ga3c_group_norm_workspace.restype = sz
     lib.ga3c_profile_read.argtypes = [vp, C.c_char_p, sz]
     _lib = lib
     return lib
@@ -519,6 +544,224 @@ def rmsprop_flat(theta, g, grad, scale: float, lr: float, rms_decay: float, rms_
     _check(load_library().ga3c_rmsprop_flat(_ptr(theta, torch.float32, "theta"), _ptr(g, torch.float32, "g"),
                                             _ptr(grad, torch.float32, "grad"), theta.numel(), scale, lr, rms_decay,
                                             rms_eps, _stream(stream)), "ga3c_rmsprop_flat")
+
+
+# ------------------------------------------------------------- memory of an agent --
+
+def _on_device(t, what: str) -> None:
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise Ga3cError(f"{what}: expected a GPU tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise Ga3cError(f"{what}: on {t.device}, which is not the current device")
+
+
+def _element_type(t, what: str) -> int:
+    import torch
+    _on_device(t, what)
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise Ga3cError(f"{what}: expected dtype torch.float32 or torch.bfloat16, got {t.dtype}")
+    return 0 if t.dtype == torch.float32 else 1
+
+
+def _heads(t, like, dim: int, what: str):
+    """View of a tensor [tokens, heads, dim] of the type and leading sizes of `like`, elements of a row side by side."""
+    _on_device(t, what)
+    if t.dtype != like.dtype:
+        raise Ga3cError(f"{what}: expected dtype {like.dtype}, got {t.dtype}")
+    if tuple(t.shape) != (like.shape[0], like.shape[1], dim):
+        raise Ga3cError(f"{what}: expected shape {(like.shape[0], like.shape[1], dim)}, got {tuple(t.shape)}")
+    if t.stride(2) != 1 and dim > 1:
+        raise Ga3cError(f"{what}: the elements of a row must lie side by side")
+    return _Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _flat(t, dtype, shape, what: str):
+    """Device pointer of a contiguous tensor of this shape; None stays None."""
+    if t is None:
+        return None
+    _on_device(t, what)
+    if tuple(t.shape) != tuple(shape):
+        raise Ga3cError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype, what)
+
+
+def _given_stream(stream, t):
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream()
+    if stream.device != t.device:
+        raise Ga3cError(f"stream: on {stream.device}, the tensors on {t.device}")
+    return stream
+
+
+def _workspace(nbytes: int, stream):
+    """Scratch that belongs to the stream which uses it (the allocator hands it out again in that stream's order)."""
+    import torch
+    if nbytes == 0:
+        return None
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
+def _decay_desc(q, v, decay, scale: float) -> _DecayDesc:
+    for t, what in ((q, "q"), (v, "v")):
+        dtype = _element_type(t, what)
+        if t.dim() != 3:
+            raise Ga3cError(f"{what}: expected [tokens, heads, dim], got {tuple(t.shape)}")
+    if len(decay) != q.shape[1]:
+        raise Ga3cError(f"decay: expected one for each of {q.shape[1]} heads, got {len(decay)}")
+    host = (C.c_float * len(decay))(*[float(d) for d in decay])
+    return _DecayDesc(q.shape[1], q.shape[2], v.shape[2], dtype, C.cast(host, C.POINTER(C.c_float)), scale)
+
+
+def _segments(q, seg_start, segments, starts):
+    """Number of segments, and the device pointers of their table and of the starts."""
+    import torch
+    n = int(q.shape[0])
+    if seg_start is not None:
+        if seg_start.dim() != 1 or seg_start.numel() < 1:
+            raise Ga3cError("seg_start: expected [segments + 1]")
+        if segments is not None and segments != seg_start.numel() - 1:
+            raise Ga3cError(f"segments: {segments}, but seg_start has {seg_start.numel() - 1}")
+        segments = seg_start.numel() - 1
+    elif segments is None:
+        segments = 1 if n else 0
+    return segments, _flat(seg_start, torch.int32, (segments + 1,), "seg_start"), _flat(starts, torch.uint8, (n,), "starts")
+
+
+def decay_attention(q, k, v, decay, out, seg_start=None, segments: Optional[int] = None, starts=None, state_in=None,
+                    state_out=None, scale: float = 1.0, stream=None) -> None:
+    """Attention with a decay for each head over segments laid end to end (ga3c_decay_attention).
+
+    q, k [tokens, heads, key_dim]; v, out [tokens, heads, value_dim], float32 or bfloat16, the elements of a row side by side;
+    decay: a number in [0, 1] for each head, on the host.  seg_start i32 [segments + 1] (GPU tensor), or None: `segments`
+    segments of equal length (one unless given).  starts u8 [tokens] or None; state_in, state_out f32 [segments, heads,
+    value_dim, key_dim] or None.  out and state_out are filled."""
+    import torch
+    lib = load_library()
+    d = _decay_desc(q, v, decay, scale)
+    n, h, dk, dv = q.shape[0], d.n_heads, d.key_dim, d.value_dim
+    segments, table, begun = _segments(q, seg_start, segments, starts)
+    state = (segments, h, dv, dk)
+    s = _given_stream(stream, q)
+    views = [_heads(q, q, dk, "q"), _heads(k, q, dk, "k"), _heads(v, q, dv, "v"), _heads(out, q, dv, "out")]
+    given = [_flat(state_in, torch.float32, state, "state_in"), _flat(state_out, torch.float32, state, "state_out")]
+    nbytes = lib.ga3c_decay_attention_workspace(C.byref(d), segments, n)
+    ws = _workspace(nbytes, s)
+    _check(lib.ga3c_decay_attention(C.byref(d), *[C.byref(x) for x in views], table, begun, segments, n, *given,
+                                    None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_decay_attention")
+
+
+def decay_attention_grad(q, k, v, decay, dout, dq, dk, dv, seg_start=None, segments: Optional[int] = None, starts=None,
+                         state_in=None, dstate_out=None, dstate_in=None, scale: float = 1.0, stream=None) -> None:
+    """Gradient of decay_attention: fills dq, dk, dv (shaped like q, k, v) and, if given, dstate_in, from dout and, if given,
+    dstate_out.  The other arguments are those of the forward call."""
+    import torch
+    lib = load_library()
+    d = _decay_desc(q, v, decay, scale)
+    n, h, kd, vd = q.shape[0], d.n_heads, d.key_dim, d.value_dim
+    segments, table, begun = _segments(q, seg_start, segments, starts)
+    state = (segments, h, vd, kd)
+    s = _given_stream(stream, q)
+    views = [_heads(q, q, kd, "q"), _heads(k, q, kd, "k"), _heads(v, q, vd, "v"), _heads(dout, q, vd, "dout"),
+             _heads(dq, q, kd, "dq"), _heads(dk, q, kd, "dk"), _heads(dv, q, vd, "dv")]
+    given = [_flat(state_in, torch.float32, state, "state_in"), _flat(dstate_out, torch.float32, state, "dstate_out"),
+             _flat(dstate_in, torch.float32, state, "dstate_in")]
+    nbytes = lib.ga3c_decay_attention_workspace(C.byref(d), segments, n)
+    ws = _workspace(nbytes, s)
+    _check(lib.ga3c_decay_attention_grad(C.byref(d), *[C.byref(x) for x in views], table, begun, segments, n, *given,
+                                         None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_decay_attention_grad")
+
+
+def decay_attention_step(q, k, v, decay, states, out, slots=None, starts=None, scale: float = 1.0, stream=None) -> None:
+    """One token of each agent (ga3c_decay_attention_step): q, k [n, heads, key_dim]; v, out [n, heads, value_dim]; states f32
+    [slots, heads, value_dim, key_dim], advanced in place; slots i32 [n] or None (token i has state i); starts u8 [n] or None."""
+    import torch
+    d = _decay_desc(q, v, decay, scale)
+    n, h, dk, dv = q.shape[0], d.n_heads, d.key_dim, d.value_dim
+    s = _given_stream(stream, q)
+    views = [_heads(q, q, dk, "q"), _heads(k, q, dk, "k"), _heads(v, q, dv, "v"), _heads(out, q, dv, "out")]
+    if not isinstance(states, torch.Tensor) or states.dim() != 4:
+        raise Ga3cError("states: expected a GPU tensor [slots, heads, value_dim, key_dim]")
+    n_slots = int(states.shape[0])
+    _check(load_library().ga3c_decay_attention_step(C.byref(d), *[C.byref(x) for x in views], _flat(slots, torch.int32, (n,), "slots"),
+                                                    _flat(starts, torch.uint8, (n,), "starts"), n,
+                                                    _flat(states, torch.float32, (n_slots, h, dv, dk), "states"), n_slots,
+                                                    s.cuda_stream), "ga3c_decay_attention_step")
+
+
+_ACT = {"none": 0, "relu": 1, "silu": 2}
+
+
+def _rows(t, like, what: str):
+    """Device pointer and position stride of [samples, ..., channels], positions evenly spaced through all samples."""
+    _on_device(t, what)
+    if t.dtype != like.dtype or t.shape != like.shape:
+        raise Ga3cError(f"{what}: expected {like.dtype} {tuple(like.shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.numel() == 0:
+        return C.c_void_p(t.data_ptr()), max(1, t.shape[-1])
+    stride, count = None, 1
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size > 1:
+            if stride is None:
+                stride = step
+            if step != stride * count:
+                raise Ga3cError(f"{what}: positions must be evenly spaced")
+        count *= size
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise Ga3cError(f"{what}: the channels of a position must lie side by side")
+    return C.c_void_p(t.data_ptr()), stride if stride is not None else t.shape[-1]
+
+
+def _norm_desc(x, groups: int, act: str, eps: float):
+    dtype = _element_type(x, "x")
+    if x.dim() < 2:
+        raise Ga3cError(f"x: expected [samples, ..., channels], got {tuple(x.shape)}")
+    if act not in _ACT:
+        raise Ga3cError(f"act: expected one of {sorted(_ACT)}, got {act!r}")
+    positions = 1
+    for size in x.shape[1:-1]:
+        positions *= int(size)
+    return _NormDesc(x.shape[-1], groups, dtype, _ACT[act], eps), int(x.shape[0]), positions
+
+
+def group_norm(x, gamma, beta, groups: int, y, stats=None, act: str = "none", eps: float = 1e-5, stream=None) -> None:
+    """Group norm with an activation ("none", "relu" or "silu"), channels last (ga3c_group_norm).
+
+    x, y [samples, ..., channels], float32 or bfloat16, positions evenly spaced; gamma, beta f32 [channels]; stats f32
+    [samples, groups, 2] or None.  y and stats (mean and 1 / standard deviation) are filled."""
+    import torch
+    lib = load_library()
+    d, samples, positions = _norm_desc(x, groups, act, eps)
+    s = _given_stream(stream, x)
+    xp, xs = _rows(x, x, "x")
+    yp, ys = _rows(y, x, "y")
+    weights = [_flat(t, torch.float32, (d.channels,), what) for t, what in ((gamma, "gamma"), (beta, "beta"))]
+    st = _flat(stats, torch.float32, (samples, groups, 2), "stats")
+    nbytes = lib.ga3c_group_norm_workspace(C.byref(d), samples, positions)
+    ws = _workspace(nbytes, s)
+    _check(lib.ga3c_group_norm(C.byref(d), xp, xs, *weights, yp, ys, st, samples, positions,
+                               None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_group_norm")
+
+
+def group_norm_grad(x, dy, gamma, beta, stats, groups: int, dx, dgamma, dbeta, act: str = "none", stream=None) -> None:
+    """Gradient of group_norm: fills dx (shaped like x), dgamma and dbeta f32 [channels] from dy and the forward call's stats."""
+    import torch
+    lib = load_library()
+    d, samples, positions = _norm_desc(x, groups, act, 0.0)
+    s = _given_stream(stream, x)
+    xp, xs = _rows(x, x, "x")
+    yp, ys = _rows(dy, x, "dy")
+    dp, ds = _rows(dx, x, "dx")
+    f = torch.float32
+    weights = [_flat(gamma, f, (d.channels,), "gamma"), _flat(beta, f, (d.channels,), "beta"),
+               _flat(stats, f, (samples, groups, 2), "stats")]
+    dw = [_flat(dgamma, f, (d.channels,), "dgamma"), _flat(dbeta, f, (d.channels,), "dbeta")]
+    nbytes = lib.ga3c_group_norm_workspace(C.byref(d), samples, positions)
+    ws = _workspace(nbytes, s)
+    _check(lib.ga3c_group_norm_grad(C.byref(d), xp, xs, yp, ys, *weights, dp, ds, *dw, samples, positions,
+                                    None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_group_norm_grad")
 
 
 def stats_from_tensor(t) -> Dict[str, float]:

@@ -1,0 +1,30 @@
+// Attention with a decay for each head (ga3c_decay_attention, _grad, _step) as the library itself calls it.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "../../include/ga3c.h"
+
+namespace ga3c {
+
+// One pass over the segments.  Forward in time (back == 0), with a state X of [rows][cols] per segment and head:
+//     X = start ? 0 : X;  X = decay X + row_t col_t^T;  out_t = out_scale X by_t
+// and backward (back == 1), from the last token of a segment to its first:
+//     Y = X + col_scale row_t col_t^T;  out_t = out_scale Y by_t;  X = start ? 0 : decay Y
+// `row` has the output's width, `col` and `by` the other one.  The output of the operator and each of its three gradients are
+// passes of this kind: (row, col, by) = (v, k, q) gives out, (k, v, dout) dq, backward (dout, q, k) dv, and (q, dout, v) dk.
+struct DecayView { void *data; int64_t token, head; };      // strides in elements
+struct DecayPass {
+    DecayView row, col, by, out;
+    int rows, cols;
+    const int32_t *seg_start;        // nullptr: segments of `len` tokens each
+    const uint8_t *starts;           // nullptr: none
+    const float *x_in;               // nullptr: zero
+    float *x_out;                    // nullptr: not wanted
+    int x_turned;                    // states lie in memory as [cols][rows]
+    int n_segments, n_tokens, len;
+    int back;
+    float out_scale, col_scale;
+    float decay[GA3C_MAX_HEADS];
+};
+
+}  // namespace ga3c

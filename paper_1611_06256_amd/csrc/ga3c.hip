@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/ga3c.h"
+#include "call_error.hpp"
 #include "frame_table.hpp"
 #include "problems.hpp"
 #include "conv_frame.hpp"
@@ -112,6 +113,14 @@ static int fail(int code, const char *fmt, ...) {
     } while (0)
 
 extern "C" const char *ga3c_last_error(void) { return g_err; }
+
+int ga3c::call_fail(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
 
 // ---------------------------------------------------------------- context ---
 
