@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "call_error.hpp"
 #include "decay_attention.hpp"
@@ -15,7 +16,7 @@ namespace ga3c {
 namespace {
 
 // Tokens of segment `seg`, kept within the arrays whatever the table says.
-__device__ inline void segment_tokens(const DecayPass &p, int seg, int &first, int &end) {
+__device__ inline void segment_tokens(const DecayJob &p, int seg, int &first, int &end) {
     if (p.seg_start) {
         first = min(max(p.seg_start[seg], 0), p.n_tokens);
         end = min(max(p.seg_start[seg + 1], first), p.n_tokens);
@@ -28,18 +29,23 @@ __device__ inline void segment_tokens(const DecayPass &p, int seg, int &first, i
 template <class T>
 __device__ inline const T *at(const DecayView &v, int token, int head) { return (const T *)v.data + token * v.token + head * v.head; }
 
-// Token by token.  A block takes DR_ROWS / LPR... rows of one segment's state in one head: LPR lanes share a row, four (or twice
-// four) columns each, and a lane has DR_RPL rows.
+// Token by token.  A block takes ROWS rows of one segment's state in one head: LPR lanes share a row, four (or twice four) columns
+// each, and a lane has DR_RPL rows.
 constexpr int DR_RPL = 4;
 template <class T, int LPR, int CV>
-__global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayPass p, int vec) {
+__global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job, int slices) {
     constexpr int RW = 64 / LPR, ROWS = 4 * RW * DR_RPL;
+    const DecayPass &p = job.pass[blockIdx.z / slices];
     const int seg = blockIdx.x, head = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int heads = gridDim.y, c0 = lane % LPR * 4, r0 = blockIdx.z * ROWS + wave * RW * DR_RPL + lane / LPR;
-    const float d = p.decay[head];
+    const int heads = gridDim.y, c0 = lane % LPR * 4, r0 = blockIdx.z % slices * ROWS + wave * RW * DR_RPL + lane / LPR;
+    const float d = job.decay[head];
     int first, end;
-    segment_tokens(p, seg, first, end);
+    segment_tokens(job, seg, first, end);
+    if (end - first > job.brief) return;
+    const int vec = (((uintptr_t)p.col.data | (uintptr_t)p.by.data) % (4 * sizeof(T)) == 0) &&
+                    ((p.col.token | p.col.head | p.by.token | p.by.head) % 4 == 0);
     const size_t state = ((size_t)seg * heads + head) * p.rows * p.cols;
+    const bool turned = p.turned, back = p.back;
     float4 x[DR_RPL][CV];
 #pragma unroll
     for (int i = 0; i < DR_RPL; ++i)
@@ -50,13 +56,13 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayPass p,
             if (p.x_in && r < p.rows)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (c + k < p.cols) e[k] = p.x_in[state + (p.x_turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)];
+                    if (c + k < p.cols) e[k] = p.x_in[state + (turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)];
             x[i][v] = float4{e[0], e[1], e[2], e[3]};
         }
     for (int n = first; n < end; ++n) {
-        const int t = p.back ? end - 1 - (n - first) : n;
-        const bool start = p.starts && p.starts[t];
-        float keep = p.back ? 1.f : start ? 0.f : d;
+        const int t = back ? end - 1 - (n - first) : n;
+        const bool start = job.starts && job.starts[t];
+        const float keep = back ? 1.f : start ? 0.f : d;
         float4 col[CV], by[CV];
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
@@ -76,7 +82,7 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayPass p,
                 y.x = keep * y.x + row * col[v].x; y.y = keep * y.y + row * col[v].y;
                 y.z = keep * y.z + row * col[v].z; y.w = keep * y.w + row * col[v].w;
                 sum += y.x * by[v].x + y.y * by[v].y + y.z * by[v].z + y.w * by[v].w;
-                if (p.back) {
+                if (back) {
                     const float f = start ? 0.f : d;
                     y = f == 0.f ? float4{0.f, 0.f, 0.f, 0.f} : float4{f * y.x, f * y.y, f * y.z, f * y.w};
                 }
@@ -96,8 +102,395 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayPass p,
             if (r < p.rows)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (c + k < p.cols) p.x_out[state + (p.x_turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)] = e[k];
+                    if (c + k < p.cols) p.x_out[state + (turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)] = e[k];
         }
+}
+
+// ---------------------------------------------------------------- chunked form --
+//
+// A block takes a span of one segment in one head, tile by tile of C positions (in the order of the pass).  With w(e) = decay^e,
+// positions i, j of the tile, n of them, and `fresh` the latest start at or before i:
+//     P[i][j] = (by_i . col_j) w(i - j)            for fresh <= j <= i, else 0
+//     out_i   = sum_j P[i][j] row_j + w(i + a) X by_i     the second term if no start is at or before i (a = 1, backward 0)
+//     X      <- w(n) X + sum_j row_j col_j w(n - j - a)   likewise
+// All four products run on the matrix instruction.  X stays in the accumulators, whose layout (four neighbouring columns of a
+// row per lane) is that of the left operand of X by_i, so it never passes through LDS; each wavefront has a quarter of the rows.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+// A fragment is 16 bytes of a row: KB numbers of the contraction in all, VE of them in one lane.
+template <class T> struct Tile;
+template <> struct Tile<float> {
+    static constexpr int C = 32, KB = 16, VE = 4, TERMS = 1;
+    typedef f32x4 Frag;
+    typedef f32x4 Quad;
+    __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+    __device__ static Quad quad(f32x4 v) { return v; }
+};
+template <> struct Tile<bf16> {
+    static constexpr int C = 64, KB = 32, VE = 8, TERMS = 3;
+    typedef bf16x8 Frag;
+    typedef bf16x4 Quad;
+    __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    __device__ static Quad quad(f32x4 v) { return __builtin_convertvector(v, bf16x4); }
+};
+
+template <class T, int CP, int RP>
+struct ChunkLds {
+    typedef Tile<T> W;
+    static constexpr int NT = CP > 64 || RP > 64 ? 512 : 256;                // threads: sixteen rows of the state per wavefront
+    static constexpr int PAD = W::VE, CB = CP + PAD, JB = W::C + PAD;        // pitches: 16 bytes more, so that rows start in other banks
+    static constexpr int BY = 0, COL = BY + W::C * CB, ROWT = COL + W::C * CB, P = ROWT + RP * JB, COLT = P + W::C * JB;
+    static constexpr int COLT_SIZE = CP * JB;
+    static constexpr size_t bytes(int terms) { return sizeof(T) * (COLT + terms * COLT_SIZE) + sizeof(float) * (W::C + 2) + sizeof(int); }
+};
+
+// Nothing is left of what is multiplied with zero, whatever it was.
+__device__ inline f32x4 scaled(f32x4 v, float w) {
+    const f32x4 r = v * w;
+    return f32x4{w == 0.f ? 0.f : r[0], w == 0.f ? 0.f : r[1], w == 0.f ? 0.f : r[2], w == 0.f ? 0.f : r[3]};
+}
+__device__ inline double power(double d, int e) {
+    double r = 1.0;
+    for (; e > 0; e >>= 1, d *= d)
+        if (e & 1) r *= d;
+    return r;
+}
+
+// Which segment and which span of it the item is; false: none.  A wavefront looks at 64 places of the table at a time.
+__device__ inline bool find_item(const DecayJob &p, int item, int &seg, int &span) {
+    if (!p.seg_start) {
+        const int each = p.len / p.span + 1;
+        seg = item / each; span = item % each;
+        return seg < p.n_segments;
+    }
+    const int lane = threadIdx.x % 64;
+    int lo = 0, hi = p.n_segments;                         // the last segment whose items begin at or before this one
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const bool before = i < hi && min(max(p.seg_start[min(i, p.n_segments)], 0), p.n_tokens) / p.span + i <= item;
+        const int k = max(1, __popcll(__ballot(before)));
+        lo += (k - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    seg = lo;
+    span = item - (min(max(p.seg_start[seg], 0), p.n_tokens) / p.span + seg);
+    return span >= 0;
+}
+
+// VE elements of a row from element `i` on, zero behind its `dim` ones (VE at least).  Rows begin anywhere: the load need not be
+// aligned, and it never leaves the row.
+template <class T>
+__device__ inline uint4 load_unit(const T *row, int i, int dim, bool ragged) {
+    constexpr int VE = Tile<T>::VE;
+    const int from = min(i, dim - VE);
+    uint4 v;
+    __builtin_memcpy(&v, row + from, 16);
+    if (ragged) {
+        const int bits = (i - from) * 8 * (int)sizeof(T);
+        uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+        if (bits >= 64) { lo = bits >= 128 ? 0 : hi >> (bits - 64); hi = 0; }
+        else if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+        v = uint4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    }
+    return v;
+}
+__device__ inline bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// MAIN: outputs, and the state behind the segment.  Otherwise the state that each span but a segment's last one makes of nothing,
+// which decay_spans_kernel turns into the states between the spans.
+template <class T, int CP, int RP, bool MAIN>
+__global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
+    typedef Tile<T> W;
+    typedef ChunkLds<T, CP, RP> L;
+    constexpr int C = W::C, KB = W::KB, VE = W::VE, IT = C / 16, CT = CP / 16, NT = L::NT, WAVES = NT / 64;
+    constexpr int COLU = C / 4 * (CP / VE), ROWU = C / 4 * (RP / VE), UNITS = COLU + ROWU + (MAIN ? COLU : 0), NU = (UNITS + NT - 1) / NT;
+    extern __shared__ uint4 lds4[];
+    T *const lds = (T *)lds4;
+    const DecayPass &p = job.pass[blockIdx.z];
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16, l16 = lane % 16;
+    static_assert(COLU % 64 == 0 && ROWU % 64 == 0, "a wavefront's units are of one tensor");
+    const int item = blockIdx.x, head = blockIdx.y, heads = gridDim.y;
+    int seg, nth, first, end;
+    if (!find_item(job, item, seg, nth)) return;
+    segment_tokens(job, seg, first, end);
+    const int whole = end - first;
+    if (whole <= job.brief || nth > whole / job.span) return;
+    const int from = nth * job.span;
+    if (nth > 0 && from >= whole) return;
+    if (!MAIN && from + job.span >= whole) return;
+    const int to = min(whole, from + job.span);                     // positions of the segment
+    const bool back = p.back, turned = p.turned, last = to == whole;
+    const int rows = p.rows, cols = p.cols, a = back ? 0 : 1;
+    const int terms = W::TERMS > 1 && p.x_out ? W::TERMS : 1;       // of a key with its decay; states are fp32 where they are handed out
+    float *const pw = (float *)(lds + L::COLT + terms * L::COLT_SIZE);
+    int *const odd = (int *)(pw + C + 2);
+    const float d = job.decay[head];
+    if (tid <= C) pw[tid] = (float)power((double)d, tid);
+    if (tid == 0) *odd = 0;
+
+    // the state: tile ct holds X[r][.] of row r = 16 wave + l16 and the four columns from 16 ct + 4 g on
+    const size_t size = (size_t)rows * cols;
+    const int row_step = turned ? 1 : cols, col_step = turned ? rows : 1;
+    const float *x_in = nth > 0 && MAIN ? p.spans + ((size_t)(item - 1) * heads + head) * size
+                                        : MAIN && p.x_in ? p.x_in + ((size_t)seg * heads + head) * size : nullptr;
+    f32x4 x[CT];
+    const int r = 16 * wave + l16;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        const int c = 16 * ct + 4 * g;
+        if (x_in)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool there = r < rows && c + e < cols;
+                const float w = x_in[there ? (uint32_t)(r * row_step + (c + e) * col_step) : 0u];
+                v[e] = there ? w : 0.f;
+            }
+        x[ct] = v;
+    }
+
+    const bool ragged = cols % VE || rows % VE || cols < CP || rows < RP;
+    const bool vec_out = (uintptr_t)p.out.data % (4 * sizeof(T)) == 0 && ((p.out.token | p.out.head | rows) % 4) == 0;
+    auto token = [&](int pos) { return back ? end - 1 - pos : first + pos; };
+    uint4 pre[NU][4];
+    int flag = 0;
+    // positions base .. base + n - 1, four neighbours and 16 bytes of each per unit
+    auto fetch = [&](int base, int n) {
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u0 = 64 * wave + NT * k;
+            if (u0 >= UNITS) break;
+            const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
+            const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
+            const int chunks = is_row ? RP / VE : CP / VE, chunk = u % chunks, q = u / chunks;
+            const DecayView &v = is_col ? p.col : is_row ? p.row : p.by;
+            const int dim = is_row ? rows : cols;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int pos = 4 * q + e;
+                pre[k][e] = pos < n ? load_unit(at<T>(v, token(base + pos), head), chunk * VE, dim, ragged) : uint4{0, 0, 0, 0};
+            }
+        }
+        if (job.starts) {
+            const int pos = base + lane, t = token(pos);
+            // backward, the cut lies between a token and the one behind it
+            flag = lane < n && (back ? pos > 0 && job.starts[t + 1] : job.starts[t]);
+        }
+    };
+    bool passes = true;                                             // whether the state in front of the span reaches its end
+    const bool mine = wave < RP / 16;
+    int base = from, single = 0;
+    fetch(base, min(C, to - base));
+    while (base < to) {
+        const int n = single ? 1 : min(C, to - base);
+        const uint64_t cuts = job.starts ? __ballot(flag) : 0;
+        const int cut = cuts ? 63 - __clzll(cuts) : -1;             // the tile's last start
+        if (base == from) __syncthreads();                          // pw
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u0 = 64 * wave + NT * k;
+            if (u0 >= UNITS) break;
+            const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
+            const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
+            const int chunks = is_row ? RP / VE : CP / VE, chunk = u % chunks, q = u / chunks;
+            union { uint4 v[4]; T e[4][VE]; } in;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) in.v[e] = pre[k][e];
+            if (!is_row && MAIN) {
+                T *at_row = lds + (is_col ? L::COL : L::BY) + 4 * q * L::CB + chunk * VE;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *(uint4 *)(at_row + e * L::CB) = in.v[e];
+            }
+            if (is_col) {
+                float f[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 4 * q + e;
+                    f[e] = j < n && j >= cut ? pw[n - j - a] * p.col_scale : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    T *at_col = lds + L::COLT + (chunk * VE + i) * L::JB + 4 * q;
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = f[e] == 0.f ? 0.f : f[e] * to_f32(in.e[e][i]);
+                    for (int term = 0;; ++term) {
+                        const typename W::Quad w = W::quad(v);
+                        *(typename W::Quad *)(at_col + term * L::COLT_SIZE) = w;
+                        if (term + 1 >= terms) break;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] -= (float)w[e];
+                    }
+                }
+            }
+            if (is_row) {
+                bool wrong = false;
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    typename W::Quad w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { w[e] = in.e[e][i]; wrong |= not_finite(to_f32(in.e[e][i])); }
+                    *(typename W::Quad *)(lds + L::ROWT + (chunk * VE + i) * L::JB + 4 * q) = w;
+                }
+                if (wrong && !single) *odd = 1;
+            }
+        }
+        __syncthreads();
+        // A product with zero does not hide a number that is not finite from the positions that must not see it: one position at
+        // a time then.
+        if (!single && n > 1 && *odd) {
+            __syncthreads();
+            if (tid == 0) *odd = 0;
+            single = n;
+            fetch(base, 1);
+            continue;
+        }
+        const int left = single > 0 ? single - 1 : 0, next = base + n;
+        if (next < to) fetch(next, left > 0 ? 1 : min(C, to - next));
+
+        typename W::Frag rowf[C / KB];
+        if (mine)
+#pragma unroll
+                for (int k = 0; k < C / KB; ++k)
+                    rowf[k] = *(const typename W::Frag *)(lds + L::ROWT + (16 * wave + l16) * L::JB + k * KB + g * VE);
+        f32x4 acc[IT];
+        if constexpr (MAIN) {
+            // scores, a 16x16 tile at a time: tile (jt, it) with jt <= it
+#pragma unroll
+            for (int k = 0; k < (IT * (IT + 1) / 2 + 3) / 4; ++k) {
+                const int t = wave + 4 * k;
+                if (t >= IT * (IT + 1) / 2) break;
+                const int it = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, jt = t - it * (it + 1) / 2;
+                f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < CP / KB; ++c) {
+                    const auto fa = *(const typename W::Frag *)(lds + L::COL + (16 * jt + l16) * L::CB + c * KB + g * VE);
+                    const auto fb = *(const typename W::Frag *)(lds + L::BY + (16 * it + l16) * L::CB + c * KB + g * VE);
+                    s = W::mma(fa, fb, s);
+                }
+                const int i = 16 * it + l16;
+                const uint64_t before = cuts & (~0ull >> (63 - i));
+                const int fresh = before ? 63 - __clzll(before) : -1;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 16 * jt + 4 * g + e;
+                    const float w = j <= i && j >= fresh ? pw[max(i - j, 0)] * p.col_scale : 0.f;
+                    s[e] = w == 0.f ? 0.f : s[e] * w;
+                }
+                *(typename W::Quad *)(lds + L::P + i * L::JB + 16 * jt + 4 * g) = W::quad(s);
+                // the fragment above the diagonal that shares a contraction step with this tile
+                if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(lds + L::P + i * L::JB + 16 * (jt + 1) + 4 * g) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+            // what the state says
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                if (!mine) break;
+                acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const T *by = lds + L::BY + (16 * it + l16) * L::CB + 4 * g;
+#pragma unroll
+                for (int c = 0; c < CP / KB; ++c) {
+                    typename W::Frag fb;
+                    if constexpr (KB == 16) fb = *(const typename W::Frag *)(by + c * KB);
+                    else {
+                        const bf16x4 lo = *(const bf16x4 *)(by + c * KB), hi = *(const bf16x4 *)(by + c * KB + 16);
+                        fb = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+                    typename W::Frag fa;
+                    if constexpr (KB == 16) fa = x[c];
+                    else {       // the state rounded to bfloat16: as an output is in the end
+                        const bf16x4 lo = W::quad(x[2 * c % CT]), hi = W::quad(x[(2 * c + 1) % CT]);
+                        fa = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+                    acc[it] = W::mma(fa, fb, acc[it]);
+                }
+                const int i = 16 * it + l16;
+                const float w = cuts & (~0ull >> (63 - i)) ? 0.f : pw[min(i + a, C)];
+                acc[it] = scaled(acc[it], w);
+            }
+            __syncthreads();
+        }
+        if (mine) {
+            if constexpr (MAIN) {
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+#pragma unroll
+                    for (int k = 0; k * KB <= 16 * it; ++k) {
+                        const auto fb = *(const typename W::Frag *)(lds + L::P + (16 * it + l16) * L::JB + k * KB + g * VE);
+                        acc[it] = W::mma(rowf[k], fb, acc[it]);
+                    }
+                    const int pos = 16 * it + l16;
+                    if (pos < n) {
+                        T *out = (T *)p.out.data + token(base + pos) * p.out.token + head * p.out.head;
+                        const int o = 16 * wave + 4 * g;
+                        const typename W::Quad w = W::quad(acc[it] * p.out_scale);
+                        if (vec_out) {
+                            if (o < rows) *(typename W::Quad *)(out + o) = w;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (o + e < rows) out[o + e] = w[e];
+                        }
+                    }
+                }
+            }
+            const float carry = cuts ? 0.f : pw[n];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+                x[ct] = scaled(x[ct], carry);
+            for (int term = 0; term < terms; ++term)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int k = 0; k < C / KB; ++k) {
+                        const auto fa = *(const typename W::Frag *)(lds + L::COLT + term * L::COLT_SIZE + (16 * ct + l16) * L::JB + k * KB + g * VE);
+                        x[ct] = W::mma(fa, rowf[k], x[ct]);
+                    }
+        }
+        passes = passes && cuts == 0;
+        __syncthreads();
+        base = next; single = left;
+    }
+    float *x_out = !MAIN ? p.spans + ((size_t)item * heads + head) * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
+    if (!MAIN && tid == 0) p.spans[(size_t)job.items * heads * size + (size_t)item * heads + head] = passes ? 1.f : 0.f;
+    if (!x_out || !mine) return;
+    const bool nothing = MAIN && back && whole > 0 && job.starts && job.starts[first];      // the first token knows of no state
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int c = 16 * ct + 4 * g;
+        if (r < rows)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < cols) x_out[(uint32_t)(r * row_step + (c + e) * col_step)] = nothing ? 0.f : x[ct][e];
+    }
+}
+
+// The states between the spans of a segment, from the segment's first state and what each span made of nothing: in place.
+__global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, int parts) {
+    const DecayPass &p = job.pass[blockIdx.z / parts];
+    const int seg = blockIdx.x, head = blockIdx.y, heads = gridDim.y;
+    int first, end;
+    segment_tokens(job, seg, first, end);
+    const int spans = (end - first + job.span - 1) / job.span;
+    if (spans < 2 || end - first <= job.brief) return;
+    const int e = (blockIdx.z % parts) * 256 + threadIdx.x;
+    const size_t size = (size_t)p.rows * p.cols;
+    if (e >= (int)size) return;
+    const int item = job.seg_start ? first / job.span + seg : seg * (job.len / job.span + 1);
+    float *at_span = p.spans + ((size_t)item * heads + head) * size + e;
+    const float *passes = p.spans + (size_t)job.items * heads * size + (size_t)item * heads + head;
+    const float w = (float)power((double)job.decay[head], job.span);
+    float x = p.x_in ? p.x_in[((size_t)seg * heads + head) * size + e] : 0.f;
+    for (int i = 0; i + 1 < spans; ++i) {
+        const float f = passes[(size_t)i * heads] * w;
+        x = (f == 0.f ? 0.f : f * x) + at_span[(size_t)i * heads * size];
+        at_span[(size_t)i * heads * size] = x;
+    }
 }
 
 // One token of each agent.  The state of entry i is row slots[i] of the states (i without slots), read, advanced and written back;
@@ -202,14 +595,101 @@ hipError_t by_columns(int cols, F go) {      // LPR, CV
     return go(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
 }
 
+// Token by token: the passes of the job, all with rows and columns of the same sizes.
 template <class T>
-hipError_t run_pass(const DecayPass &p, int heads, hipStream_t s) {
-    const int vec = rows_of_four<T>(p.col) && rows_of_four<T>(p.by);
-    return by_columns(p.cols, [&](auto lpr, auto cv) {
+hipError_t launch_recurrent(const DecayJob &job, int passes, int heads, hipStream_t s) {
+    return by_columns(job.pass[0].cols, [&](auto lpr, auto cv) {
         constexpr int ROWS = 4 * (64 / lpr.value) * DR_RPL;
-        launch(decay_recurrent_kernel<T, lpr.value, cv.value>, dim3(p.n_segments, heads, (p.rows + ROWS - 1) / ROWS), dim3(256), 0, s, p, vec);
+        const int slices = (job.pass[0].rows + ROWS - 1) / ROWS;
+        launch(decay_recurrent_kernel<T, lpr.value, cv.value>, dim3(job.n_segments, heads, passes * slices), dim3(256), 0, s, job, slices);
         return hipGetLastError();
     });
+}
+
+template <class T, int CP, int RP, bool MAIN>
+hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipStream_t s) {
+    static size_t lds_set = 0;
+    bool exact = false;
+    for (int i = 0; i < passes; ++i) exact = exact || job.pass[i].x_out;
+    const size_t lds = ChunkLds<T, CP, RP>::bytes(exact ? Tile<T>::TERMS : 1);
+    if (lds > 64 * 1024 && lds > lds_set) {
+        const hipError_t e = hipFuncSetAttribute((const void *)decay_chunk_kernel<T, CP, RP, MAIN>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        lds_set = lds;
+    }
+    launch(decay_chunk_kernel<T, CP, RP, MAIN>, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP>::NT), lds, s, job);
+    return hipGetLastError();
+}
+template <class T, bool MAIN>
+hipError_t launch_chunk(const DecayJob &job, int passes, int heads, hipStream_t s) {
+    auto with_cols = [&](auto cp) {
+        const int rows = job.pass[0].rows;
+        if (rows <= 32) return launch_chunk_kernel<T, cp.value, 32, MAIN>(job, passes, heads, s);
+        if (rows <= 64) return launch_chunk_kernel<T, cp.value, 64, MAIN>(job, passes, heads, s);
+        return launch_chunk_kernel<T, cp.value, 128, MAIN>(job, passes, heads, s);
+    };
+    const int cols = job.pass[0].cols;
+    if (cols <= 32) return with_cols(std::integral_constant<int, 32>());
+    if (cols <= 64) return with_cols(std::integral_constant<int, 64>());
+    return with_cols(std::integral_constant<int, 128>());
+}
+
+// Calls go(job, passes) for each group of passes with the same sizes of rows and columns.
+template <class F>
+hipError_t by_sizes(const DecayJob &job, int passes, F go) {
+    bool done[3] = {false, false, false};
+    for (int i = 0; i < passes; ++i) {
+        if (done[i]) continue;
+        DecayJob some = job;
+        int n = 0;
+        for (int k = i; k < passes; ++k)
+            if (!done[k] && job.pass[k].rows == job.pass[i].rows && job.pass[k].cols == job.pass[i].cols) { some.pass[n++] = job.pass[k]; done[k] = true; }
+        const hipError_t e = go(some, n);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Tokens that a block of the chunked kernels takes.  Spans of a segment cost its keys and values read twice and two states each,
+// so there are no more of them than it takes to give every compute unit a block.
+int span_of(int heads, int n_segments, int n_tokens) {
+    const int64_t want = (int64_t)n_tokens * heads / 256;
+    return (int)std::min<int64_t>(1 << 20, std::max<int64_t>(256, (want + 63) / 64 * 64));
+}
+// Segments of up to so many tokens take the token-by-token kernel if the average is short.
+constexpr int BRIEF = 32;
+
+// Rows shorter than a load of the chunked kernels.
+constexpr int NARROW = 8;
+
+void plan(DecayJob &job, int heads, int key, int value) {
+    job.span = span_of(heads, job.n_segments, job.n_tokens);
+    job.items = job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
+    job.brief = std::min(key, value) < NARROW ? INT32_MAX : job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
+}
+size_t spans_floats(const DecayJob &job, int heads, size_t size) {
+    const int longest = job.seg_start ? job.n_tokens : job.len;
+    return longest <= job.span || longest <= job.brief ? 0 : (size_t)job.items * heads * (size + 1);
+}
+
+// passes: of outputs; sources: those of them whose spans' states are made (one forward, one backward)
+template <class T>
+hipError_t run_job(DecayJob &job, int passes, const int *sources, int n_sources, int heads, hipStream_t s) {
+    const int longest = job.seg_start ? job.n_tokens : job.len;
+    hipError_t e = hipSuccess;
+    if (job.brief >= 0 && (job.seg_start || longest <= job.brief))
+        e = by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_recurrent<T>(some, n, heads, s); });
+    if (e != hipSuccess || (job.brief >= 0 && longest <= job.brief)) return e;
+    if (longest > job.span) {
+        DecayJob made = job;
+        for (int i = 0; i < n_sources; ++i) made.pass[i] = job.pass[sources[i]];
+        e = by_sizes(made, n_sources, [&](const DecayJob &some, int n) { return launch_chunk<T, false>(some, n, heads, s); });
+        if (e != hipSuccess) return e;
+        const int parts = (job.pass[0].rows * job.pass[0].cols + 255) / 256;
+        launch(decay_spans_kernel, dim3(job.n_segments, heads, parts * n_sources), dim3(256), 0, s, made, parts);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    return by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_chunk<T, true>(some, n, heads, s); });
 }
 
 int check_desc(const ga3c_decay_desc *d, const char *who) {
@@ -248,6 +728,7 @@ int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *
 }
 int check_segments(const int32_t *seg_start, int n_segments, int n_tokens, const char *who) {
     if (n_segments < 0 || n_tokens < 0) return call_fail(GA3C_EINVAL, "%s: negative count", who);
+    if (n_segments > 1 << 30) return call_fail(GA3C_EINVAL, "%s: more than 2^30 segments", who);
     if (n_segments == 0 && n_tokens > 0) return call_fail(GA3C_EINVAL, "%s: tokens without a segment", who);
     if (!seg_start && n_segments > 0 && n_tokens % n_segments) return call_fail(GA3C_EINVAL, "%s: %d tokens are no %d equal segments", who, n_tokens, n_segments);
     return GA3C_OK;
@@ -257,17 +738,21 @@ bool overlap(const void *a, const void *b, size_t bytes) {
 }
 DecayView view(const ga3c_heads *h) { return h ? DecayView{h->data, h->token_stride, h->head_stride} : DecayView{nullptr, 0, 0}; }
 
-DecayPass pass_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_t *starts, int n_segments, int n_tokens) {
-    DecayPass p;
-    memset(&p, 0, sizeof p);
-    p.seg_start = seg_start; p.starts = starts; p.n_segments = n_segments; p.n_tokens = n_tokens;
-    p.len = n_segments > 0 ? n_tokens / n_segments : 0;
-    p.out_scale = d->scale; p.col_scale = 1.f;
-    memcpy(p.decay, d->decay, sizeof(float) * d->n_heads);
-    return p;
+DecayJob job_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_t *starts, int n_segments, int n_tokens) {
+    DecayJob j;
+    memset(&j, 0, sizeof j);
+    j.seg_start = seg_start; j.starts = starts; j.n_segments = n_segments; j.n_tokens = n_tokens;
+    j.len = n_tokens / n_segments;
+    memcpy(j.decay, d->decay, sizeof(float) * d->n_heads);
+    plan(j, d->n_heads, d->key_dim, d->value_dim);
+    return j;
 }
-hipError_t run(const ga3c_decay_desc *d, const DecayPass &p, hipStream_t s) {
-    return d->dtype == GA3C_BF16 ? run_pass<bf16>(p, d->n_heads, s) : run_pass<float>(p, d->n_heads, s);
+DecayPass pass_of(const ga3c_heads *row, const ga3c_heads *col, const ga3c_heads *by, const ga3c_heads *out, int rows, int cols, int turned, int back,
+                  float out_scale, float col_scale, const float *x_in, float *x_out, float *spans) {
+    return DecayPass{view(row), view(col), view(by), view(out), rows, cols, turned, back, out_scale, col_scale, x_in, x_out, spans};
+}
+hipError_t run(const ga3c_decay_desc *d, DecayJob &j, int passes, const int *sources, int n_sources, hipStream_t s) {
+    return d->dtype == GA3C_BF16 ? run_job<bf16>(j, passes, sources, n_sources, d->n_heads, s) : run_job<float>(j, passes, sources, n_sources, d->n_heads, s);
 }
 int hip_result(hipError_t e, const char *who) { return e == hipSuccess ? GA3C_OK : call_fail(GA3C_EHIP, "%s: %s", who, hipGetErrorString(e)); }
 
@@ -277,8 +762,10 @@ int hip_result(hipError_t e, const char *who) { return e == hipSuccess ? GA3C_OK
 using namespace ga3c;
 
 extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n_segments, int n_tokens) {
-    (void)d; (void)n_segments; (void)n_tokens;
-    return 0;
+    if (check_desc(d, "ga3c_decay_attention_workspace") != GA3C_OK || n_segments < 1 || n_tokens < 1) return 0;
+    // as with a table, which needs the most; the gradient has states of both directions
+    const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens);
+    return 2 * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
 }
 
 extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
@@ -296,13 +783,13 @@ extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *
         if (rc != GA3C_OK) return rc;
     }
     if (overlap(state_in, state_out, state)) return call_fail(GA3C_EINVAL, "%s: state_out lies over state_in", who);
-    if (workspace_bytes < ga3c_decay_attention_workspace(d, n_segments, n_tokens)) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
-    (void)workspace;
-    DecayPass p = pass_of(d, seg_start, starts, n_segments, n_tokens);
-    p.row = view(v); p.col = view(k); p.by = view(q); p.out = view(out);
-    p.rows = d->value_dim; p.cols = d->key_dim;
-    p.x_in = state_in; p.x_out = state_out;
-    return hip_result(run(d, p, (hipStream_t)stream), who);
+    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens);
+    if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
+    if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
+    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);
+    j.pass[0] = pass_of(v, k, q, out, d->value_dim, d->key_dim, 0, 0, d->scale, 1.f, state_in, state_out, (float *)workspace);
+    const int sources[] = {0};
+    return hip_result(run(d, j, 1, sources, 1, (hipStream_t)stream), who);
 }
 
 extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
@@ -321,23 +808,18 @@ extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_he
         if (rc != GA3C_OK) return rc;
     }
     if (overlap(state_in, dstate_in, state) || overlap(dstate_out, dstate_in, state)) return call_fail(GA3C_EINVAL, "%s: dstate_in lies over an input", who);
-    if (workspace_bytes < ga3c_decay_attention_workspace(d, n_segments, n_tokens)) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
-    (void)workspace;
-    const hipStream_t s = (hipStream_t)stream;
-    DecayPass p = pass_of(d, seg_start, starts, n_segments, n_tokens);
-    // dq: the states in front of the tokens once more, read out by dout
-    p.row = view(k); p.col = view(v); p.by = view(dout); p.out = view(dq);
-    p.rows = d->key_dim; p.cols = d->value_dim; p.x_turned = 1; p.x_in = state_in; p.x_out = nullptr;
-    hipError_t e = run(d, p, s);
-    // the gradient of the state behind each token, read out by v and by k
-    p.back = 1; p.out_scale = 1.f; p.col_scale = d->scale;
-    p.x_in = dstate_out;
-    p.row = view(q); p.col = view(dout); p.by = view(v); p.out = view(dk);
-    if (e == hipSuccess) e = run(d, p, s);
-    p.rows = d->value_dim; p.cols = d->key_dim; p.x_turned = 0; p.x_out = dstate_in;
-    p.row = view(dout); p.col = view(q); p.by = view(k); p.out = view(dv);
-    if (e == hipSuccess) e = run(d, p, s);
-    return hip_result(e, who);
+    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens);
+    if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
+    if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
+    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);
+    const int key = d->key_dim, value = d->value_dim;
+    float *forward = (float *)workspace, *backward = forward + spans_floats(j, d->n_heads, (size_t)key * value);
+    // the states in front of the tokens once more, read out by dout; the gradient of the state behind each token, read out by v and k
+    j.pass[0] = pass_of(k, v, dout, dq, key, value, 1, 0, d->scale, 1.f, state_in, nullptr, forward);
+    j.pass[1] = pass_of(q, dout, v, dk, key, value, 1, 1, 1.f, d->scale, dstate_out, nullptr, backward);
+    j.pass[2] = pass_of(dout, q, k, dv, value, key, 0, 1, 1.f, d->scale, dstate_out, dstate_in, backward);
+    const int sources[] = {0, 2};         // the one that knows whether dstate_in is wanted, and its states in 32 bits
+    return hip_result(run(d, j, 3, sources, 2, (hipStream_t)stream), who);
 }
 
 extern "C" int ga3c_decay_attention_step(const ga3c_decay_desc *d, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,

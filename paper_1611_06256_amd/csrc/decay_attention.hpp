@@ -1,4 +1,4 @@
-// Attention with a decay for each head (ga3c_decay_attention, _grad, _step) as the library itself calls it.
+// What the passes of decay_attention.hip compute, and how they are described to the kernels.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -16,14 +16,21 @@ struct DecayView { void *data; int64_t token, head; };      // strides in elemen
 struct DecayPass {
     DecayView row, col, by, out;
     int rows, cols;
-    const int32_t *seg_start;        // nullptr: segments of `len` tokens each
-    const uint8_t *starts;           // nullptr: none
-    const float *x_in;               // nullptr: zero
-    float *x_out;                    // nullptr: not wanted
-    int x_turned;                    // states lie in memory as [cols][rows]
-    int n_segments, n_tokens, len;
+    int turned;                      // states lie in memory as [cols][rows]
     int back;
     float out_scale, col_scale;
+    const float *x_in;               // nullptr: zero
+    float *x_out;                    // nullptr: not wanted
+    float *spans;                    // states between the spans of a segment, and behind them whether a span passes its own on
+};
+struct DecayJob {
+    DecayPass pass[3];               // one grid: a pass per z
+    const int32_t *seg_start;        // nullptr: segments of `len` tokens each
+    const uint8_t *starts;           // nullptr: none
+    int n_segments, n_tokens, len;
+    int span;                        // tokens of a segment that one block of the chunked kernels takes
+    int items;                       // places for spans: those of segment i begin at seg_start[i] / span + i
+    int brief;                       // segments of up to so many tokens go to the token-by-token kernel, longer ones to the chunked
     float decay[GA3C_MAX_HEADS];
 };
 

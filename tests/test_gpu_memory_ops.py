@@ -69,6 +69,8 @@ CASES = [
     ([90, 33], 2, 8, 127, True, 0.05, [0.0, 0.98], False),
     ([700], 1, 32, 64, True, 0.002, [0.998], False),
     ([1100, 3, 900], 2, 64, 48, True, 0.001, [0.99, 0.9995], False),
+    ([1] * 60 + [300] + [2] * 40, 2, 32, 16, True, 0.01, [0.97, 0.5], False),      # short ones and a long one
+    ([1, 2, 3, 70, 4, 0], 3, 100, 20, False, None, [0.9, 0.8, 1.0], True),
 ]
 
 
@@ -153,6 +155,44 @@ def test_a_start_hides_whatever_came_before():
         g.decay_attention(s["q"], s["k"], s["v"], decay, got[0], starts=starts, state_in=s["state_in"], state_out=got[1])
         torch.cuda.synchronize()
         assert torch.equal(got[0][cut:], clean[0][cut:]) and torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[20], [90], [600]], ids=["20", "90", "600"])
+def test_numbers_that_are_not_finite_stay_where_they_belong(lens, dtype):
+    # a token that is not finite reaches neither the tokens before it nor, past a start, those behind it; nor other segments
+    lens = lens + [17]
+    h, dk, dv, decay, n = 2, 32, 48, [0.9, 0.99], lens[0]
+    bad, cut = n // 3, n // 2
+    s = make(lens, h, dk, dv, dtype, True, None, False)
+    s["starts"] = torch.zeros(sum(lens), dtype=torch.uint8, device="cuda")
+    s["starts"][cut] = 1
+    w = {k: wide(v) for k, v in s.items()}
+    size = {k: v.abs() if k not in ("starts", "seg_start") else v for k, v in w.items()}
+    s["v"][bad, 0, 5] = float("inf")
+    s["k"][bad + 1, 1, 7] = float("nan")
+    s["q"][bad + 2, 0, 3] = float("nan")
+    s["dout"][bad + 3, 1, 2] = float("-inf")
+    out, state = torch.empty(sum(lens), h, dv, dtype=dtype, device="cuda"), torch.empty(2, h, dv, dk, device="cuda")
+    kw = dict(seg_start=s["seg_start"], starts=s["starts"], state_in=s["state_in"])
+    g.decay_attention(s["q"], s["k"], s["v"], decay, out, state_out=state, **kw)
+    grads = [torch.empty_like(s[x]) for x in "qkv"] + [torch.empty_like(state)]
+    g.decay_attention_grad(s["q"], s["k"], s["v"], decay, s["dout"], *grads[:3], dstate_out=s["dstate_out"], dstate_in=grads[3], **kw)
+    torch.cuda.synchronize()
+    factors = 2 * n + dk + dv + 24
+    want = ref.attention(w["q"], w["k"], w["v"], decay, lens, w["starts"], w["state_in"])
+    mags = ref.attention(size["q"], size["k"], size["v"], decay, lens, w["starts"], size["state_in"])
+    for part in (slice(0, bad), slice(cut, None)):
+        near(out[part], want[0][part], mags[0][part], factors, f"out {part}", dtype)
+    near(state, want[1], mags[1], factors, "state_out")
+    assert not torch.isfinite(out[bad]).all()
+    want = ref.attention_grad(w["q"], w["k"], w["v"], decay, lens, w["dout"], w["starts"], w["state_in"], w["dstate_out"])
+    mags = ref.attention_grad(size["q"], size["k"], size["v"], decay, lens, size["dout"], w["starts"], size["state_in"], size["dstate_out"])
+    for got, a, m, what in zip(grads, want, mags, ("dq", "dk", "dv")):
+        near(got[cut:], a[cut:], m[cut:], factors, what, dtype)
+        if what == "dq":
+            near(got[:bad], a[:bad], m[:bad], factors, what, dtype)
+    near(grads[3][1], want[3][1], mags[3][1], factors, "dstate_in")
 
 
 def test_a_bad_table_stays_within_the_arrays():
