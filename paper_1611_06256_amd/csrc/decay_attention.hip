@@ -121,7 +121,13 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // A fragment is 16 bytes of a row: KB numbers of the contraction in all, VE of them in one lane.
 template <class T> struct Tile;
-template <> struct Tile<float> {
+// The units of a tensor's tile (four positions, 16 bytes of each) in a wavefront's lanes: eight units side by side in a row, a
+// memory line, then the next four positions.
+template <int C> struct Units {
+    __device__ static int chunk(int u, int chunks) { const int w = min(8, chunks); return u % w + u / (w * (C / 4)) * w; }
+    __device__ static int quad_of(int u, int chunks) { return u / min(8, chunks) % (C / 4); }
+};
+template <> struct Tile<float> : Units<32> {
     static constexpr int C = 32, KB = 16, VE = 4, TERMS = 1;
     typedef f32x4 Frag;
     typedef f32x4 Quad;
@@ -132,7 +138,7 @@ template <> struct Tile<float> {
     }
     __device__ static Quad quad(f32x4 v) { return v; }
 };
-template <> struct Tile<bf16> {
+template <> struct Tile<bf16> : Units<64> {
     static constexpr int C = 64, KB = 32, VE = 8, TERMS = 3;
     typedef bf16x8 Frag;
     typedef bf16x4 Quad;
@@ -147,9 +153,19 @@ struct ChunkLds {
     static constexpr int PAD = W::VE, CB = CP + PAD, JB = W::C + PAD;        // pitches: 16 bytes more, so that rows start in other banks
     static constexpr int BY = 0, COL = BY + W::C * CB, ROWT = COL + W::C * CB, P = ROWT + RP * JB, COLT = P + W::C * JB;
     static constexpr int COLT_SIZE = CP * JB;
+    // Place of a position in a row of the turned images.  Eight rows of bfloat16 are half a turn of the banks: every second sixteen
+    // rows lie the other way round, so that the four positions of 64 units reach all banks.
+    __device__ static int turned(int row, int j) { return row * JB + (sizeof(T) == 2 ? j ^ (row / 16 % 2 * 32) : j); }
     static constexpr size_t bytes(int terms) { return sizeof(T) * (COLT + terms * COLT_SIZE) + sizeof(float) * (W::C + 2) + sizeof(int); }
 };
 
+// The lane's number as if it were new: places that are made of it are worked out where they are used, not kept in registers from
+// one tile to the next (the bfloat16 kernel of 128 columns: 237 registers with them, and one block per compute unit).
+__device__ inline int fresh_lane() {
+    int lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 // Nothing is left of what is multiplied with zero, whatever it was.
 __device__ inline f32x4 scaled(f32x4 v, float w) {
     const f32x4 r = v * w;
@@ -183,28 +199,42 @@ __device__ inline bool find_item(const DecayJob &p, int item, int &seg, int &spa
     return span >= 0;
 }
 
-// VE elements of a row from element `i` on, zero behind its `dim` ones (VE at least).  Rows begin anywhere: the load need not be
-// aligned, and it never leaves the row.
+// VE elements of a row from element `i` on, or as many from where the row's last VE begin: the load need not be aligned, never
+// leaves the row, and nothing waits for it here.  in_place() then moves elements that came too far up to their places, with
+// zeros behind the row's `dim` elements (VE at least).
 template <class T>
-__device__ inline uint4 load_unit(const T *row, int i, int dim, bool ragged) {
-    constexpr int VE = Tile<T>::VE;
-    const int from = min(i, dim - VE);
+__device__ inline uint4 load_unit(const T *row, int i, int dim) {
     uint4 v;
-    __builtin_memcpy(&v, row + from, 16);
-    if (ragged) {
-        const int bits = (i - from) * 8 * (int)sizeof(T);
-        uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
-        if (bits >= 64) { lo = bits >= 128 ? 0 : hi >> (bits - 64); hi = 0; }
-        else if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
-        v = uint4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-    }
+    __builtin_memcpy(&v, row + min(i, dim - Tile<T>::VE), 16);
     return v;
 }
-__device__ inline bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+template <class T>
+__device__ inline uint4 in_place(uint4 v, int i, int dim) {
+    const int bits = (i - min(i, dim - Tile<T>::VE)) * 8 * (int)sizeof(T);
+    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+    if (bits >= 64) { lo = bits >= 128 ? 0 : hi >> (bits - 64); hi = 0; }
+    else if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+    return uint4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+// Whether one of the numbers in 64 bytes has an exponent of ones.
+template <class T>
+__device__ inline bool not_finite(const uint4 (&v)[4]) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        for (uint32_t w : {v[e].x, v[e].y, v[e].z, v[e].w}) {
+            if constexpr (sizeof(T) == 4) most = max(most, w & 0x7fffffffu);
+            else most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+        }
+    if constexpr (sizeof(T) == 4) return most >= 0x7f800000u;
+    return (most >> 16) >= 0x7f80u || (most & 0xffffu) >= 0x7f80u;
+}
 
 // MAIN: outputs, and the state behind the segment.  Otherwise the state that each span but a segment's last one makes of nothing,
 // which decay_spans_kernel turns into the states between the spans.
-template <class T, int CP, int RP, bool MAIN>
+// TERMS: of a key with its decay in the state's sum.
+template <class T, int CP, int RP, bool MAIN, int TERMS>
 __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
     typedef Tile<T> W;
     typedef ChunkLds<T, CP, RP> L;
@@ -227,8 +257,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
     const int to = min(whole, from + job.span);                     // positions of the segment
     const bool back = p.back, turned = p.turned, last = to == whole;
     const int rows = p.rows, cols = p.cols, a = back ? 0 : 1;
-    const int terms = W::TERMS > 1 && p.x_out ? W::TERMS : 1;       // of a key with its decay; states are fp32 where they are handed out
-    float *const pw = (float *)(lds + L::COLT + terms * L::COLT_SIZE);
+    float *const pw = (float *)(lds + L::COLT + TERMS * L::COLT_SIZE);
     int *const odd = (int *)(pw + C + 2);
     const float d = job.decay[head];
     if (tid <= C) pw[tid] = (float)power((double)d, tid);
@@ -241,11 +270,13 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                                         : MAIN && p.x_in ? p.x_in + ((size_t)seg * heads + head) * size : nullptr;
     f32x4 x[CT];
     const int r = 16 * wave + l16;
+    const bool quads = !turned && cols % 4 == 0 && (uintptr_t)x_in % 16 == 0;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         f32x4 v{0.f, 0.f, 0.f, 0.f};
         const int c = 16 * ct + 4 * g;
-        if (x_in)
+        if (x_in && quads) v = r < rows && c < cols ? *(const f32x4 *)(x_in + (uint32_t)(r * cols + c)) : v;
+        else if (x_in)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bool there = r < rows && c + e < cols;
@@ -262,46 +293,64 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
     int flag = 0;
     // positions base .. base + n - 1, four neighbours and 16 bytes of each per unit
     auto fetch = [&](int base, int n) {
+        const int lowest = back ? end - base - n : first + base;     // the tile's first token in memory
+        const int lane = fresh_lane();
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u0 = 64 * wave + NT * k;
             if (u0 >= UNITS) break;
             const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
             const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
-            const int chunks = is_row ? RP / VE : CP / VE, chunk = u % chunks, q = u / chunks;
+            const int chunk = W::chunk(u, is_row ? RP / VE : CP / VE), q = W::quad_of(u, is_row ? RP / VE : CP / VE);
             const DecayView &v = is_col ? p.col : is_row ? p.row : p.by;
+            const T *tile = at<T>(v, lowest, head);
+            const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
             const int dim = is_row ? rows : cols;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int pos = 4 * q + e;
-                pre[k][e] = pos < n ? load_unit(at<T>(v, token(base + pos), head), chunk * VE, dim, ragged) : uint4{0, 0, 0, 0};
+                const int pos = min(4 * q + e, n - 1);
+                pre[k][e] = load_unit((const T *)((const char *)tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * step), chunk * VE, dim);
             }
         }
         if (job.starts) {
-            const int pos = base + lane, t = token(pos);
             // backward, the cut lies between a token and the one behind it
-            flag = lane < n && (back ? pos > 0 && job.starts[t + 1] : job.starts[t]);
+            const int t = token(base + min(lane, n - 1)) + (back ? 1 : 0);
+            flag = job.starts[min(t, end - 1)];
         }
     };
     bool passes = true;                                             // whether the state in front of the span reaches its end
-    const bool mine = wave < RP / 16;
+    const bool mine = RP / 16 == WAVES || wave < RP / 16;
     int base = from, single = 0;
-    fetch(base, min(C, to - base));
+    if (base < to) fetch(base, min(C, to - base));
+    __syncthreads();                                                // pw
     while (base < to) {
-        const int n = single ? 1 : min(C, to - base);
-        const uint64_t cuts = job.starts ? __ballot(flag) : 0;
+        int n;
+        uint64_t cuts;
+        for (bool again = false;; again = true) {
+        n = again || single ? 1 : min(C, to - base);
+        const int lane = fresh_lane();
+        cuts = job.starts ? __ballot(lane < n && flag && !(back && base + lane == 0)) : 0;
         const int cut = cuts ? 63 - __clzll(cuts) : -1;             // the tile's last start
-        if (base == from) __syncthreads();                          // pw
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u0 = 64 * wave + NT * k;
             if (u0 >= UNITS) break;
             const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
             const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
-            const int chunks = is_row ? RP / VE : CP / VE, chunk = u % chunks, q = u / chunks;
+            const int chunk = W::chunk(u, is_row ? RP / VE : CP / VE), q = W::quad_of(u, is_row ? RP / VE : CP / VE);
             union { uint4 v[4]; T e[4][VE]; } in;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) in.v[e] = pre[k][e];
+            for (int e = 0; e < 4; ++e) {
+                in.v[e] = pre[k][e];
+                // what is made of a load is made here: further up, it would wait for the load
+                asm volatile("" : "+v"(in.v[e].x), "+v"(in.v[e].y), "+v"(in.v[e].z), "+v"(in.v[e].w));
+            }
+            if (ragged)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) in.v[e] = in_place<T>(in.v[e], chunk * VE, is_row ? rows : cols);
+            if (n < C)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) in.v[e] = 4 * q + e < n ? in.v[e] : uint4{0, 0, 0, 0};
             if (!is_row && MAIN) {
                 T *at_row = lds + (is_col ? L::COL : L::BY) + 4 * q * L::CB + chunk * VE;
 #pragma unroll
@@ -310,33 +359,32 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
             if (is_col) {
                 float f[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = 4 * q + e;
-                    f[e] = j < n && j >= cut ? pw[n - j - a] * p.col_scale : 0.f;
-                }
+                for (int e = 0; e < 4; ++e) f[e] = pw[max(n - (4 * q + e) - a, 0)] * p.col_scale;
+                if (cuts)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) in.v[e] = 4 * q + e >= cut ? in.v[e] : uint4{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
-                    T *at_col = lds + L::COLT + (chunk * VE + i) * L::JB + 4 * q;
+                    T *at_col = lds + L::COLT + L::turned(chunk * VE + i, 4 * q);
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = f[e] == 0.f ? 0.f : f[e] * to_f32(in.e[e][i]);
-                    for (int term = 0;; ++term) {
+                    for (int e = 0; e < 4; ++e) v[e] = f[e] * to_f32(in.e[e][i]);
+#pragma unroll
+                    for (int term = 0; term < TERMS; ++term) {
                         const typename W::Quad w = W::quad(v);
                         *(typename W::Quad *)(at_col + term * L::COLT_SIZE) = w;
-                        if (term + 1 >= terms) break;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] -= (float)w[e];
+                        if (term + 1 < TERMS) v -= __builtin_convertvector(w, f32x4);
                     }
                 }
             }
             if (is_row) {
-                bool wrong = false;
+                const bool wrong = not_finite<T>(in.v);
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
                     typename W::Quad w;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { w[e] = in.e[e][i]; wrong |= not_finite(to_f32(in.e[e][i])); }
-                    *(typename W::Quad *)(lds + L::ROWT + (chunk * VE + i) * L::JB + 4 * q) = w;
+                    for (int e = 0; e < 4; ++e) w[e] = in.e[e][i];
+                    *(typename W::Quad *)(lds + L::ROWT + L::turned(chunk * VE + i, 4 * q)) = w;
                 }
                 if (wrong && !single) *odd = 1;
             }
@@ -344,27 +392,28 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
         __syncthreads();
         // A product with zero does not hide a number that is not finite from the positions that must not see it: one position at
         // a time then.
-        if (!single && n > 1 && *odd) {
-            __syncthreads();
-            if (tid == 0) *odd = 0;
-            single = n;
-            fetch(base, 1);
-            continue;
+        if (single || n == 1 || !*odd) break;
+        __syncthreads();
+        if (tid == 0) *odd = 0;
+        single = n;
+        fetch(base, 1);
         }
-        const int left = single > 0 ? single - 1 : 0, next = base + n;
-        if (next < to) fetch(next, left > 0 ? 1 : min(C, to - next));
+        base += n;
+        single = max(single - 1, 0);
+        if (base < to) fetch(base, single ? 1 : min(C, to - base));
 
         typename W::Frag rowf[C / KB];
         if (mine)
 #pragma unroll
                 for (int k = 0; k < C / KB; ++k)
-                    rowf[k] = *(const typename W::Frag *)(lds + L::ROWT + (16 * wave + l16) * L::JB + k * KB + g * VE);
+                    rowf[k] = *(const typename W::Frag *)(lds + L::ROWT + L::turned(16 * wave + l16, k * KB + g * VE));
         f32x4 acc[IT];
         if constexpr (MAIN) {
             // scores, a 16x16 tile at a time: tile (jt, it) with jt <= it
 #pragma unroll
-            for (int k = 0; k < (IT * (IT + 1) / 2 + 3) / 4; ++k) {
-                const int t = wave + 4 * k;
+            for (int k = 0; k < (IT * (IT + 1) / 2 + WAVES - 1) / WAVES; ++k) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int t = wave + WAVES * k;
                 if (t >= IT * (IT + 1) / 2) break;
                 const int it = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, jt = t - it * (it + 1) / 2;
                 f32x4 s{0.f, 0.f, 0.f, 0.f};
@@ -388,37 +437,46 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                 if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(lds + L::P + i * L::JB + 16 * (jt + 1) + 4 * g) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
             }
             // what the state says
+            if (mine) {
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                if (!mine) break;
-                acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
-                const T *by = lds + L::BY + (16 * it + l16) * L::CB + 4 * g;
+                for (int it = 0; it < IT; ++it) acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < CP / KB; ++c) {
-                    typename W::Frag fb;
-                    if constexpr (KB == 16) fb = *(const typename W::Frag *)(by + c * KB);
-                    else {
-                        const bf16x4 lo = *(const bf16x4 *)(by + c * KB), hi = *(const bf16x4 *)(by + c * KB + 16);
-                        fb = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    __builtin_amdgcn_sched_barrier(0);      // loads of all steps at once would not fit the registers
+                    const T *by = lds + L::BY + l16 * L::CB + c * KB + 4 * g;
+                    if constexpr (KB == 16) {
+#pragma unroll
+                        for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], *(const typename W::Frag *)(by + 16 * it * L::CB), acc[it]);
+                    } else {       // two terms of the state, 16 bits: one alone doubles the error of the result's own rounding
+                        const f32x4 x0 = x[2 * c % CT], x1 = x[(2 * c + 1) % CT];
+                        const bf16x4 h0 = W::quad(x0), h1 = W::quad(x1);
+                        const bf16x4 l0 = W::quad(x0 - __builtin_convertvector(h0, f32x4)), l1 = W::quad(x1 - __builtin_convertvector(h1, f32x4));
+                        const bf16x8 h = __builtin_shufflevector(h0, h1, 0, 1, 2, 3, 4, 5, 6, 7), l = __builtin_shufflevector(l0, l1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                        for (int it = 0; it < IT; ++it) {
+                            const bf16x4 b0 = *(const bf16x4 *)(by + 16 * it * L::CB), b1 = *(const bf16x4 *)(by + 16 * it * L::CB + 16);
+                            const bf16x8 fb = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
+                            acc[it] = W::mma(h, fb, acc[it]);
+                            acc[it] = W::mma(l, fb, acc[it]);
+                        }
                     }
-                    typename W::Frag fa;
-                    if constexpr (KB == 16) fa = x[c];
-                    else {       // the state rounded to bfloat16: as an output is in the end
-                        const bf16x4 lo = W::quad(x[2 * c % CT]), hi = W::quad(x[(2 * c + 1) % CT]);
-                        fa = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    }
-                    acc[it] = W::mma(fa, fb, acc[it]);
                 }
-                const int i = 16 * it + l16;
-                const float w = cuts & (~0ull >> (63 - i)) ? 0.f : pw[min(i + a, C)];
-                acc[it] = scaled(acc[it], w);
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    const int i = 16 * it + l16;
+                    acc[it] = scaled(acc[it], cuts & (~0ull >> (63 - i)) ? 0.f : pw[min(i + a, C)]);
+                }
             }
             __syncthreads();
         }
         if (mine) {
             if constexpr (MAIN) {
+                // `base` is the next tile's
+                T *out_tile = (T *)at<T>(p.out, back ? end - base : first + base - n, head);
+                const uint32_t out_step = (uint32_t)p.out.token * (uint32_t)sizeof(T);
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int k = 0; k * KB <= 16 * it; ++k) {
                         const auto fb = *(const typename W::Frag *)(lds + L::P + (16 * it + l16) * L::JB + k * KB + g * VE);
@@ -426,7 +484,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                     }
                     const int pos = 16 * it + l16;
                     if (pos < n) {
-                        T *out = (T *)p.out.data + token(base + pos) * p.out.token + head * p.out.head;
+                        T *out = (T *)((char *)out_tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * out_step);
                         const int o = 16 * wave + 4 * g;
                         const typename W::Quad w = W::quad(acc[it] * p.out_scale);
                         if (vec_out) {
@@ -441,29 +499,33 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
             }
             const float carry = cuts ? 0.f : pw[n];
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-                x[ct] = scaled(x[ct], carry);
-            for (int term = 0; term < terms; ++term)
+            for (int ct = 0; ct < CT; ++ct) x[ct] = scaled(x[ct], carry);
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
+            for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int k = 0; k < C / KB; ++k) {
-                        const auto fa = *(const typename W::Frag *)(lds + L::COLT + term * L::COLT_SIZE + (16 * ct + l16) * L::JB + k * KB + g * VE);
+                        const auto fa = *(const typename W::Frag *)(lds + L::COLT + term * L::COLT_SIZE + L::turned(16 * ct + l16, k * KB + g * VE));
                         x[ct] = W::mma(fa, rowf[k], x[ct]);
                     }
+                }
         }
         passes = passes && cuts == 0;
         __syncthreads();
-        base = next; single = left;
     }
     float *x_out = !MAIN ? p.spans + ((size_t)item * heads + head) * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
     if (!MAIN && tid == 0) p.spans[(size_t)job.items * heads * size + (size_t)item * heads + head] = passes ? 1.f : 0.f;
     if (!x_out || !mine) return;
+    const bool quads_out = !turned && cols % 4 == 0 && (uintptr_t)x_out % 16 == 0;
     const bool nothing = MAIN && back && whole > 0 && job.starts && job.starts[first];      // the first token knows of no state
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int c = 16 * ct + 4 * g;
-        if (r < rows)
+        if (quads_out) {
+            if (r < rows && c < cols) *(f32x4 *)(x_out + (uint32_t)(r * cols + c)) = nothing ? f32x4{0.f, 0.f, 0.f, 0.f} : x[ct];
+        } else if (r < rows)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (c + e < cols) x_out[(uint32_t)(r * row_step + (c + e) * col_step)] = nothing ? 0.f : x[ct][e];
@@ -606,32 +668,33 @@ hipError_t launch_recurrent(const DecayJob &job, int passes, int heads, hipStrea
     });
 }
 
-template <class T, int CP, int RP, bool MAIN>
+template <class T, int CP, int RP, bool MAIN, int TERMS>
 hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipStream_t s) {
     static size_t lds_set = 0;
-    bool exact = false;
-    for (int i = 0; i < passes; ++i) exact = exact || job.pass[i].x_out;
-    const size_t lds = ChunkLds<T, CP, RP>::bytes(exact ? Tile<T>::TERMS : 1);
-    if (lds > 64 * 1024 && lds > lds_set) {
-        const hipError_t e = hipFuncSetAttribute((const void *)decay_chunk_kernel<T, CP, RP, MAIN>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    const auto kernel = decay_chunk_kernel<T, CP, RP, MAIN, TERMS>;
+    constexpr size_t lds = ChunkLds<T, CP, RP>::bytes(TERMS);
+    if (lds > 64 * 1024 && lds_set == 0) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
         lds_set = lds;
     }
-    launch(decay_chunk_kernel<T, CP, RP, MAIN>, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP>::NT), lds, s, job);
+    launch(kernel, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP>::NT), lds, s, job);
     return hipGetLastError();
+}
+// States are fp32 where they are handed out: a bfloat16 key with its decay then goes in as three terms, else as one.
+template <class T, int CP, int RP, bool MAIN>
+hipError_t launch_chunk_terms(const DecayJob &job, int passes, int heads, hipStream_t s) {
+    bool out = false;
+    for (int i = 0; i < passes; ++i) out = out || job.pass[i].x_out;
+    if constexpr (Tile<T>::TERMS > 1)
+        if (out) return launch_chunk_kernel<T, CP, RP, MAIN, Tile<T>::TERMS>(job, passes, heads, s);
+    return launch_chunk_kernel<T, CP, RP, MAIN, 1>(job, passes, heads, s);
 }
 template <class T, bool MAIN>
 hipError_t launch_chunk(const DecayJob &job, int passes, int heads, hipStream_t s) {
-    auto with_cols = [&](auto cp) {
-        const int rows = job.pass[0].rows;
-        if (rows <= 32) return launch_chunk_kernel<T, cp.value, 32, MAIN>(job, passes, heads, s);
-        if (rows <= 64) return launch_chunk_kernel<T, cp.value, 64, MAIN>(job, passes, heads, s);
-        return launch_chunk_kernel<T, cp.value, 128, MAIN>(job, passes, heads, s);
-    };
-    const int cols = job.pass[0].cols;
-    if (cols <= 32) return with_cols(std::integral_constant<int, 32>());
-    if (cols <= 64) return with_cols(std::integral_constant<int, 64>());
-    return with_cols(std::integral_constant<int, 128>());
+    const bool wide_rows = job.pass[0].rows > 64;
+    if (job.pass[0].cols > 64) return wide_rows ? launch_chunk_terms<T, 128, 128, MAIN>(job, passes, heads, s) : launch_chunk_terms<T, 128, 64, MAIN>(job, passes, heads, s);
+    return wide_rows ? launch_chunk_terms<T, 64, 128, MAIN>(job, passes, heads, s) : launch_chunk_terms<T, 64, 64, MAIN>(job, passes, heads, s);
 }
 
 // Calls go(job, passes) for each group of passes with the same sizes of rows and columns.
@@ -709,15 +772,18 @@ bool apart(const ga3c_heads &v, int n, int heads, int dim) {
     if (t < dim || h < dim) return false;
     return n <= 1 || heads <= 1 || t >= h * (heads - 1) + dim || h >= t * (n - 1) + dim;
 }
+constexpr int64_t MAX_STRIDE = 1 << 30;      // a step in bytes is a 32-bit number in the kernels
 int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *out, const int *out_dims, int n_out, int n, int heads, size_t size, const char *who) {
     for (int i = 0; i < n_in; ++i) {
         if (!in[i] || !in[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)in[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
         if (in[i]->token_stride < 0 || in[i]->head_stride < 0) return call_fail(GA3C_EINVAL, "%s: negative stride", who);
+        if (in[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^30 or more", who);
     }
     for (int i = 0; i < n_out; ++i) {
         if (!out[i] || !out[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)out[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
+        if (out[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^30 or more", who);
         if (!apart(*out[i], n, heads, out_dims[i])) return call_fail(GA3C_EINVAL, "%s: strides make rows of an output overlap", who);
         for (int k = 0; k < n_in; ++k)
             if (out[i]->data == in[k]->data) return call_fail(GA3C_EINVAL, "%s: an output is one of the inputs", who);
