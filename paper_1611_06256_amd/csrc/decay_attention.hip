@@ -114,20 +114,17 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job
 //     out_i   = sum_j P[i][j] row_j + w(i + a) X by_i     the second term if no start is at or before i (a = 1, backward 0)
 //     X      <- w(n) X + sum_j row_j col_j w(n - j - a)   likewise
 // All four products run on the matrix instruction.  X stays in the accumulators, whose layout (four neighbouring columns of a
-// row per lane) is that of the left operand of X by_i, so it never passes through LDS; each wavefront has a quarter of the rows.
+// row per lane) is that of the left operand of X by_i, so it never passes through LDS; a wavefront has sixteen of its rows.
+// The tiles go straight from memory to LDS, the next one while this one is worked on; contractions over positions read them
+// across their rows (an instruction of its own for 16 bits, single numbers for 32).
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// A fragment is 16 bytes of a row: KB numbers of the contraction in all, VE of them in one lane.
+// A fragment is 16 bytes of one lane: KB numbers of the contraction in the wavefront, VE of them in the lane.
 template <class T> struct Tile;
-// The units of a tensor's tile (four positions, 16 bytes of each) in a wavefront's lanes: eight units side by side in a row, a
-// memory line, then the next four positions.
-template <int C> struct Units {
-    __device__ static int chunk(int u, int chunks) { const int w = min(8, chunks); return u % w + u / (w * (C / 4)) * w; }
-    __device__ static int quad_of(int u, int chunks) { return u / min(8, chunks) % (C / 4); }
-};
-template <> struct Tile<float> : Units<32> {
+template <> struct Tile<float> {
     static constexpr int C = 32, KB = 16, VE = 4, TERMS = 1;
     typedef f32x4 Frag;
     typedef f32x4 Quad;
@@ -138,7 +135,7 @@ template <> struct Tile<float> : Units<32> {
     }
     __device__ static Quad quad(f32x4 v) { return v; }
 };
-template <> struct Tile<bf16> : Units<64> {
+template <> struct Tile<bf16> {
     static constexpr int C = 64, KB = 32, VE = 8, TERMS = 3;
     typedef bf16x8 Frag;
     typedef bf16x4 Quad;
@@ -146,21 +143,53 @@ template <> struct Tile<bf16> : Units<64> {
     __device__ static Quad quad(f32x4 v) { return __builtin_convertvector(v, bf16x4); }
 };
 
-template <class T, int CP, int RP>
+// One tensor's tile in LDS: C rows of D numbers, 16-byte pieces of a row in another order in each row, so that both ways of
+// reading reach all banks: the same piece of sixteen rows, and (16 bits) two neighbouring pieces of rows 0-3, 8-11, 16-19, 24-27,
+// (32 bits) four pieces of every fourth row.
+template <class T, int D>
+struct Image {
+    typedef Tile<T> W;
+    static constexpr int PIECES = D * (int)sizeof(T) / 16, BYTES = W::C * PIECES * 16;
+    __device__ static int order(int row) {
+        if (sizeof(T) == 4) return row & 15;
+        if (PIECES >= 16) return (row >> 2 & 1) | (row & 3) << 1 | (row & 8);
+        return (row >> 2 & 1) | (row & 2) | (row >> 1 & 4);
+    }
+    __device__ static int place(int row, int piece) { return (row * PIECES + (piece ^ order(row))) * 16; }
+    // numbers k .. k + VE - 1 of a row
+    __device__ static typename W::Frag along(const char *at, int row, int k) { return *(const typename W::Frag *)(at + place(row, k / W::VE)); }
+    // (bfloat16) four numbers from an even quad on
+    __device__ static bf16x4 four(const char *at, int row, int k) { return *(const bf16x4 *)(at + place(row, k / 8) + k % 8 * 2); }
+    // column first + l16 of rows j + VE g .. + VE - 1, as the lanes of an operand hold them
+    __device__ static typename W::Frag across(const char *at, int j, int first, int g, int l16) {
+        typename W::Frag f;
+        if constexpr (sizeof(T) == 4) {
+            const int c = first + l16;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = *(const float *)(at + place(j + 4 * g + e, c / 4) + c % 4 * 4);
+        } else {
+            // lanes 4 t .. 4 t + 3 give the places of a row's four quads, and lane i takes column i of the four rows
+            const int row = j + 8 * g + l16 / 4, k = first + 4 * (l16 % 4);
+            typedef __attribute__((address_space(3))) s16x4 *Lds;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + place(row, k / 8) + k % 8 * 2));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + place(row + 4, k / 8) + k % 8 * 2));
+            f = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return f;
+    }
+};
+
+template <class T, int CP, int RP, bool MAIN>
 struct ChunkLds {
     typedef Tile<T> W;
     static constexpr int NT = CP > 64 || RP > 64 ? 512 : 256;                // threads: sixteen rows of the state per wavefront
-    static constexpr int PAD = W::VE, CB = CP + PAD, JB = W::C + PAD;        // pitches: 16 bytes more, so that rows start in other banks
-    static constexpr int BY = 0, COL = BY + W::C * CB, ROWT = COL + W::C * CB, P = ROWT + RP * JB, COLT = P + W::C * JB;
-    static constexpr int COLT_SIZE = CP * JB;
-    // Place of a position in a row of the turned images.  Eight rows of bfloat16 are half a turn of the banks: every second sixteen
-    // rows lie the other way round, so that the four positions of 64 units reach all banks.
-    __device__ static int turned(int row, int j) { return row * JB + (sizeof(T) == 2 ? j ^ (row / 16 % 2 * 32) : j); }
-    static constexpr size_t bytes(int terms) { return sizeof(T) * (COLT + terms * COLT_SIZE) + sizeof(float) * (W::C + 2) + sizeof(int); }
+    static constexpr int COL = 0, ROW = COL + Image<T, CP>::BYTES, BY = ROW + Image<T, RP>::BYTES, SET = BY + (MAIN ? Image<T, CP>::BYTES : 0);
+    static constexpr int JB = W::C + W::VE;                                  // pitch of P
+    static constexpr int P = 2 * SET, PW = P + (MAIN ? W::C * JB * (int)sizeof(T) : 0), FW = PW + (W::C + 4) * 4, ODD = FW + W::C * 4, BYTES = ODD + 16;
 };
 
 // The lane's number as if it were new: places that are made of it are worked out where they are used, not kept in registers from
-// one tile to the next (the bfloat16 kernel of 128 columns: 237 registers with them, and one block per compute unit).
+// one tile to the next.
 __device__ inline int fresh_lane() {
     int lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));
@@ -199,67 +228,113 @@ __device__ inline bool find_item(const DecayJob &p, int item, int &seg, int &spa
     return span >= 0;
 }
 
-// VE elements of a row from element `i` on, or as many from where the row's last VE begin: the load need not be aligned, never
-// leaves the row, and nothing waits for it here.  in_place() then moves elements that came too far up to their places, with
-// zeros behind the row's `dim` elements (VE at least).
+// Pieces of rows that are not there.
+__device__ const uint4 decay_nothing[1] = {{0, 0, 0, 0}};
+
+// 16 bytes per lane to lds + 16 * lane; lds is the same for the whole wavefront.  The caller waits for vmcnt itself: the compiler,
+// which would wait for every such load in front of the next LDS read, does not see it.
+__device__ inline void piece_to_lds(const void *from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+}
+// VE elements of a row from element `i` on, zero behind its `dim` elements; rows begin anywhere.
 template <class T>
-__device__ inline uint4 load_unit(const T *row, int i, int dim) {
-    uint4 v;
-    __builtin_memcpy(&v, row + min(i, dim - Tile<T>::VE), 16);
-    return v;
+__device__ inline uint4 loose_piece(const T *row, int i, int dim) {
+    constexpr int VE = Tile<T>::VE;
+    union { uint4 u; T e[VE]; } r;
+    r.u = uint4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < VE; ++k)
+        if (i + k < dim) r.e[k] = row[i + k];
+    return r.u;
 }
 template <class T>
-__device__ inline uint4 in_place(uint4 v, int i, int dim) {
-    const int bits = (i - min(i, dim - Tile<T>::VE)) * 8 * (int)sizeof(T);
-    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
-    if (bits >= 64) { lo = bits >= 128 ? 0 : hi >> (bits - 64); hi = 0; }
-    else if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
-    return uint4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+__device__ inline bool whole_pieces(const DecayView &v, int dim) {
+    return (uintptr_t)v.data % 16 == 0 && ((v.token | v.head | dim) % Tile<T>::VE) == 0;
 }
-// Whether one of the numbers in 64 bytes has an exponent of ones.
+// The tile of one tensor: positions base .. base + n - 1 of the span, zeros behind them.
+template <class T, int D, int NT>
+__device__ inline void stage(const DecayView &v, int dim, bool whole, int lowest, int n, bool back, int head, char *to, int wave) {
+    typedef Image<T, D> I;
+    const int lane = fresh_lane();
+    const char *rows = (const char *)at<T>(v, lowest, head);         // the tile's first token in memory
+    const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
+    constexpr int ALL = I::BYTES / 16;
+    static_assert(ALL % 64 == 0, "whole wavefronts");
+#pragma unroll
+    for (int k = 0; k < (ALL + NT - 1) / NT; ++k) {
+        const int first = 64 * wave + NT * k;
+        if (ALL % NT && first >= ALL) break;
+        const int s = first + lane, pos = s / I::PIECES, piece = (s % I::PIECES) ^ I::order(pos), i = piece * Tile<T>::VE;
+        const char *row = rows + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * step;
+        if (whole)
+            piece_to_lds(pos < n && i < dim ? (const void *)(row + piece * 16) : (const void *)decay_nothing,
+                         __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + first * 16));
+        else {
+            uint4 u{0, 0, 0, 0};
+            if (pos < n && i < dim) u = loose_piece((const T *)row, i, dim);
+            *(uint4 *)(to + s * 16) = u;
+        }
+    }
+}
+
+// Whether one of the numbers in 16 bytes has an exponent of ones.
 template <class T>
-__device__ inline bool not_finite(const uint4 (&v)[4]) {
+__device__ inline bool not_finite(uint4 v) {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        for (uint32_t w : {v[e].x, v[e].y, v[e].z, v[e].w}) {
-            if constexpr (sizeof(T) == 4) most = max(most, w & 0x7fffffffu);
-            else most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
-        }
+    for (uint32_t w : {v.x, v.y, v.z, v.w}) {
+        if constexpr (sizeof(T) == 4) most = max(most, w & 0x7fffffffu);
+        else most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+    }
     if constexpr (sizeof(T) == 4) return most >= 0x7f800000u;
     return (most >> 16) >= 0x7f80u || (most & 0xffffu) >= 0x7f80u;
 }
 
 // MAIN: outputs, and the state behind the segment.  Otherwise the state that each span but a segment's last one makes of nothing,
-// which decay_spans_kernel turns into the states between the spans.
-// TERMS: of a key with its decay in the state's sum.
+// which decay_spans_kernel turns into the states between the spans.  TERMS: of a row with its decay in the state's sum.
 template <class T, int CP, int RP, bool MAIN, int TERMS>
-__global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
+__global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
     typedef Tile<T> W;
-    typedef ChunkLds<T, CP, RP> L;
-    constexpr int C = W::C, KB = W::KB, VE = W::VE, IT = C / 16, CT = CP / 16, NT = L::NT, WAVES = NT / 64;
-    constexpr int COLU = C / 4 * (CP / VE), ROWU = C / 4 * (RP / VE), UNITS = COLU + ROWU + (MAIN ? COLU : 0), NU = (UNITS + NT - 1) / NT;
+    typedef ChunkLds<T, CP, RP, MAIN> L;
+    typedef Image<T, CP> IC;
+    typedef Image<T, RP> IR;
+    constexpr int C = W::C, KB = W::KB, VE = W::VE, IT = C / 16, CT = CP / 16, KT = C / KB, NT = L::NT, WAVES = NT / 64;
     extern __shared__ uint4 lds4[];
-    T *const lds = (T *)lds4;
+    char *const lds = (char *)lds4;
+    T *const P = (T *)(lds + L::P);
+    float *const pw = (float *)(lds + L::PW), *const fw = (float *)(lds + L::FW);
+    int *const odd = (int *)(lds + L::ODD);
     const DecayPass &p = job.pass[blockIdx.z];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16, l16 = lane % 16;
-    static_assert(COLU % 64 == 0 && ROWU % 64 == 0, "a wavefront's units are of one tensor");
     const int item = blockIdx.x, head = blockIdx.y, heads = gridDim.y;
     int seg, nth, first, end;
     if (!find_item(job, item, seg, nth)) return;
     segment_tokens(job, seg, first, end);
+    first = __builtin_amdgcn_readfirstlane(first); end = __builtin_amdgcn_readfirstlane(end);
     const int whole = end - first;
     if (whole <= job.brief || nth > whole / job.span) return;
-    const int from = nth * job.span;
+    const int from = __builtin_amdgcn_readfirstlane(nth * job.span);
     if (nth > 0 && from >= whole) return;
     if (!MAIN && from + job.span >= whole) return;
     const int to = min(whole, from + job.span);                     // positions of the segment
     const bool back = p.back, turned = p.turned, last = to == whole;
     const int rows = p.rows, cols = p.cols, a = back ? 0 : 1;
-    float *const pw = (float *)(lds + L::COLT + TERMS * L::COLT_SIZE);
-    int *const odd = (int *)(pw + C + 2);
     const float d = job.decay[head];
+    const bool pieces = whole_pieces<T>(p.col, cols) && whole_pieces<T>(p.row, rows) && whole_pieces<T>(p.by, cols);
+    int flag = 0;
+    auto fetch = [&](int base, int n, char *set) {
+        const int lowest = back ? end - base - n : first + base;
+        stage<T, CP, NT>(p.col, cols, pieces, lowest, n, back, head, set + L::COL, wave);
+        stage<T, RP, NT>(p.row, rows, pieces, lowest, n, back, head, set + L::ROW, wave);
+        if (MAIN) stage<T, CP, NT>(p.by, cols, pieces, lowest, n, back, head, set + L::BY, wave);
+        if (job.starts) {
+            // backward, the cut lies between a token and the one behind it
+            const int pos = min(lane, n - 1), t = lowest + (back ? n - pos : pos);
+            flag = job.starts[min(t, end - 1)];
+        }
+    };
+    int base = from, single = 0, set = 0;
+    if (base < to) fetch(base, min(C, to - base), lds);
     if (tid <= C) pw[tid] = (float)power((double)d, tid);
     if (tid == 0) *odd = 0;
 
@@ -286,143 +361,44 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
         x[ct] = v;
     }
 
-    const bool ragged = cols % VE || rows % VE || cols < CP || rows < RP;
     const bool vec_out = (uintptr_t)p.out.data % (4 * sizeof(T)) == 0 && ((p.out.token | p.out.head | rows) % 4) == 0;
-    auto token = [&](int pos) { return back ? end - 1 - pos : first + pos; };
-    uint4 pre[NU][4];
-    int flag = 0;
-    // positions base .. base + n - 1, four neighbours and 16 bytes of each per unit
-    auto fetch = [&](int base, int n) {
-        const int lowest = back ? end - base - n : first + base;     // the tile's first token in memory
-        const int lane = fresh_lane();
-#pragma unroll
-        for (int k = 0; k < NU; ++k) {
-            const int u0 = 64 * wave + NT * k;
-            if (u0 >= UNITS) break;
-            const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
-            const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
-            const int chunk = W::chunk(u, is_row ? RP / VE : CP / VE), q = W::quad_of(u, is_row ? RP / VE : CP / VE);
-            const DecayView &v = is_col ? p.col : is_row ? p.row : p.by;
-            const T *tile = at<T>(v, lowest, head);
-            const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
-            const int dim = is_row ? rows : cols;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int pos = min(4 * q + e, n - 1);
-                pre[k][e] = load_unit((const T *)((const char *)tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * step), chunk * VE, dim);
-            }
-        }
-        if (job.starts) {
-            // backward, the cut lies between a token and the one behind it
-            const int t = token(base + min(lane, n - 1)) + (back ? 1 : 0);
-            flag = job.starts[min(t, end - 1)];
-        }
-    };
     bool passes = true;                                             // whether the state in front of the span reaches its end
     const bool mine = RP / 16 == WAVES || wave < RP / 16;
-    int base = from, single = 0;
-    if (base < to) fetch(base, min(C, to - base));
     __syncthreads();                                                // pw
     while (base < to) {
-        int n;
-        uint64_t cuts;
-        for (bool again = false;; again = true) {
-        n = again || single ? 1 : min(C, to - base);
-        const int lane = fresh_lane();
-        cuts = job.starts ? __ballot(lane < n && flag && !(back && base + lane == 0)) : 0;
+        const int n = single ? 1 : min(C, to - base);
+        const uint64_t cuts = job.starts ? __ballot(lane < n && flag && !(back && base + lane == 0)) : 0;
         const int cut = cuts ? 63 - __clzll(cuts) : -1;             // the tile's last start
-#pragma unroll
-        for (int k = 0; k < NU; ++k) {
-            const int u0 = 64 * wave + NT * k;
-            if (u0 >= UNITS) break;
-            const bool is_col = u0 < COLU, is_row = !is_col && u0 < COLU + ROWU;
-            const int u = u0 - (is_col ? 0 : is_row ? COLU : COLU + ROWU) + lane;
-            const int chunk = W::chunk(u, is_row ? RP / VE : CP / VE), q = W::quad_of(u, is_row ? RP / VE : CP / VE);
-            union { uint4 v[4]; T e[4][VE]; } in;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                in.v[e] = pre[k][e];
-                // what is made of a load is made here: further up, it would wait for the load
-                asm volatile("" : "+v"(in.v[e].x), "+v"(in.v[e].y), "+v"(in.v[e].z), "+v"(in.v[e].w));
-            }
-            if (ragged)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) in.v[e] = in_place<T>(in.v[e], chunk * VE, is_row ? rows : cols);
-            if (n < C)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) in.v[e] = 4 * q + e < n ? in.v[e] : uint4{0, 0, 0, 0};
-            if (!is_row && MAIN) {
-                T *at_row = lds + (is_col ? L::COL : L::BY) + 4 * q * L::CB + chunk * VE;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) *(uint4 *)(at_row + e * L::CB) = in.v[e];
-            }
-            if (is_col) {
-                float f[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = pw[max(n - (4 * q + e) - a, 0)] * p.col_scale;
-                if (cuts)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) in.v[e] = 4 * q + e >= cut ? in.v[e] : uint4{0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    T *at_col = lds + L::COLT + L::turned(chunk * VE + i, 4 * q);
-                    f32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = f[e] * to_f32(in.e[e][i]);
-#pragma unroll
-                    for (int term = 0; term < TERMS; ++term) {
-                        const typename W::Quad w = W::quad(v);
-                        *(typename W::Quad *)(at_col + term * L::COLT_SIZE) = w;
-                        if (term + 1 < TERMS) v -= __builtin_convertvector(w, f32x4);
-                    }
-                }
-            }
-            if (is_row) {
-                const bool wrong = not_finite<T>(in.v);
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    typename W::Quad w;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = in.e[e][i];
-                    *(typename W::Quad *)(lds + L::ROWT + L::turned(chunk * VE + i, 4 * q)) = w;
-                }
-                if (wrong && !single) *odd = 1;
-            }
-        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        // A product with zero does not hide a number that is not finite from the positions that must not see it: one position at
-        // a time then.
-        if (single || n == 1 || !*odd) break;
-        __syncthreads();
-        if (tid == 0) *odd = 0;
-        single = n;
-        fetch(base, 1);
-        }
-        base += n;
-        single = max(single - 1, 0);
-        if (base < to) fetch(base, single ? 1 : min(C, to - base));
+        const char *const now = lds + set;
+        char *const then = lds + (L::SET - set);
+        if (base + n < to) fetch(base + n, single > 1 ? 1 : min(C, to - base - n), then);
 
-        typename W::Frag rowf[C / KB];
+        if (tid < C) fw[tid] = tid < n && tid >= cut ? pw[n - tid - a] * p.col_scale : 0.f;
+        typename W::Frag rowf[KT], colf;
+        bool wrong = false;
         if (mine)
 #pragma unroll
-                for (int k = 0; k < C / KB; ++k)
-                    rowf[k] = *(const typename W::Frag *)(lds + L::ROWT + L::turned(16 * wave + l16, k * KB + g * VE));
+            for (int k = 0; k < KT; ++k) {
+                rowf[k] = IR::across(now + L::ROW, KB * k, 16 * wave, g, l16);
+                wrong = wrong || not_finite<T>(__builtin_bit_cast(uint4, rowf[k]));
+            }
+        if (cuts)
+            for (int s = tid; s < IC::BYTES / 16; s += NT) wrong = wrong || not_finite<T>(*(const uint4 *)(now + L::COL + 16 * s));
+        if (wrong && !single) *odd = 1;
         f32x4 acc[IT];
         if constexpr (MAIN) {
             // scores, a 16x16 tile at a time: tile (jt, it) with jt <= it
 #pragma unroll
             for (int k = 0; k < (IT * (IT + 1) / 2 + WAVES - 1) / WAVES; ++k) {
-                __builtin_amdgcn_sched_barrier(0);
                 const int t = wave + WAVES * k;
                 if (t >= IT * (IT + 1) / 2) break;
                 const int it = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, jt = t - it * (it + 1) / 2;
                 f32x4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < CP / KB; ++c) {
-                    const auto fa = *(const typename W::Frag *)(lds + L::COL + (16 * jt + l16) * L::CB + c * KB + g * VE);
-                    const auto fb = *(const typename W::Frag *)(lds + L::BY + (16 * it + l16) * L::CB + c * KB + g * VE);
-                    s = W::mma(fa, fb, s);
-                }
+                for (int c = 0; c < CP / KB; ++c)
+                    s = W::mma(IC::along(now + L::COL, 16 * jt + l16, c * KB + g * VE), IC::along(now + L::BY, 16 * it + l16, c * KB + g * VE), s);
                 const int i = 16 * it + l16;
                 const uint64_t before = cuts & (~0ull >> (63 - i));
                 const int fresh = before ? 63 - __clzll(before) : -1;
@@ -432,9 +408,9 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                     const float w = j <= i && j >= fresh ? pw[max(i - j, 0)] * p.col_scale : 0.f;
                     s[e] = w == 0.f ? 0.f : s[e] * w;
                 }
-                *(typename W::Quad *)(lds + L::P + i * L::JB + 16 * jt + 4 * g) = W::quad(s);
+                *(typename W::Quad *)(P + i * L::JB + 16 * jt + 4 * g) = W::quad(s);
                 // the fragment above the diagonal that shares a contraction step with this tile
-                if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(lds + L::P + i * L::JB + 16 * (jt + 1) + 4 * g) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
+                if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(P + i * L::JB + 16 * (jt + 1) + 4 * g) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
             }
             // what the state says
             if (mine) {
@@ -443,10 +419,9 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
 #pragma unroll
                 for (int c = 0; c < CP / KB; ++c) {
                     __builtin_amdgcn_sched_barrier(0);      // loads of all steps at once would not fit the registers
-                    const T *by = lds + L::BY + l16 * L::CB + c * KB + 4 * g;
                     if constexpr (KB == 16) {
 #pragma unroll
-                        for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], *(const typename W::Frag *)(by + 16 * it * L::CB), acc[it]);
+                        for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], IC::along(now + L::BY, 16 * it + l16, KB * c + 4 * g), acc[it]);
                     } else {       // two terms of the state, 16 bits: one alone doubles the error of the result's own rounding
                         const f32x4 x0 = x[2 * c % CT], x1 = x[(2 * c + 1) % CT];
                         const bf16x4 h0 = W::quad(x0), h1 = W::quad(x1);
@@ -454,7 +429,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                         const bf16x8 h = __builtin_shufflevector(h0, h1, 0, 1, 2, 3, 4, 5, 6, 7), l = __builtin_shufflevector(l0, l1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
                         for (int it = 0; it < IT; ++it) {
-                            const bf16x4 b0 = *(const bf16x4 *)(by + 16 * it * L::CB), b1 = *(const bf16x4 *)(by + 16 * it * L::CB + 16);
+                            const bf16x4 b0 = IC::four(now + L::BY, 16 * it + l16, KB * c + 4 * g), b1 = IC::four(now + L::BY, 16 * it + l16, KB * c + 16 + 4 * g);
                             const bf16x8 fb = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
                             acc[it] = W::mma(h, fb, acc[it]);
                             acc[it] = W::mma(l, fb, acc[it]);
@@ -467,53 +442,72 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP>::NT), 2) void decay_chunk_kern
                     acc[it] = scaled(acc[it], cuts & (~0ull >> (63 - i)) ? 0.f : pw[min(i + a, C)]);
                 }
             }
-            __syncthreads();
         }
-        if (mine) {
-            if constexpr (MAIN) {
-                // `base` is the next tile's
-                T *out_tile = (T *)at<T>(p.out, back ? end - base : first + base - n, head);
-                const uint32_t out_step = (uint32_t)p.out.token * (uint32_t)sizeof(T);
+        __syncthreads();
+        // A product with zero does not hide a number that is not finite from the positions that must not see it: one position at
+        // a time then.
+        if (!single && n > 1 && *odd) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) *odd = 0;
+            single = n;
+            fetch(base, 1, then);
+        } else {
+            if (mine) {
+                if constexpr (MAIN) {
+                    char *const out_tile = (char *)at<T>(p.out, back ? end - base - n : first + base, head);
+                    const uint32_t out_step = (uint32_t)p.out.token * (uint32_t)sizeof(T);
 #pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int it = 0; it < IT; ++it) {
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int k = 0; k * KB <= 16 * it; ++k) {
-                        const auto fb = *(const typename W::Frag *)(lds + L::P + (16 * it + l16) * L::JB + k * KB + g * VE);
-                        acc[it] = W::mma(rowf[k], fb, acc[it]);
-                    }
-                    const int pos = 16 * it + l16;
-                    if (pos < n) {
-                        T *out = (T *)((char *)out_tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * out_step);
-                        const int o = 16 * wave + 4 * g;
+                        for (int k = 0; k * KB <= 16 * it; ++k)
+                            acc[it] = W::mma(rowf[k], *(const typename W::Frag *)(P + (16 * it + l16) * L::JB + k * KB + g * VE), acc[it]);
+                        const int pos = 16 * it + l16, o = 16 * wave + 4 * g;
                         const typename W::Quad w = W::quad(acc[it] * p.out_scale);
-                        if (vec_out) {
+                        T *out = (T *)(out_tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * out_step);
+                        if (pos < n && vec_out) {
                             if (o < rows) *(typename W::Quad *)(out + o) = w;
-                        } else {
+                        } else if (pos < n) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 if (o + e < rows) out[o + e] = w[e];
                         }
                     }
                 }
-            }
-            const float carry = cuts ? 0.f : pw[n];
+                // rows with their decay, in place of the keys: a wavefront needs its own rows only
+                typename W::Frag rs[TERMS][KT];
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) x[ct] = scaled(x[ct], carry);
+                for (int k = 0; k < KT; ++k) {
+                    float v[VE];
 #pragma unroll
-            for (int term = 0; term < TERMS; ++term)
+                    for (int e = 0; e < VE; ++e) v[e] = (float)rowf[k][e] * fw[KB * k + VE * g + e];
+#pragma unroll
+                    for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) {
+                            rs[term][k][e] = from_f32<T>(v[e]);
+                            if (term + 1 < TERMS) v[e] -= (float)rs[term][k][e];
+                        }
+                }
+                const float carry = cuts ? 0.f : pw[n];
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                    x[ct] = scaled(x[ct], carry);
 #pragma unroll
-                    for (int k = 0; k < C / KB; ++k) {
-                        const auto fa = *(const typename W::Frag *)(lds + L::COLT + term * L::COLT_SIZE + L::turned(16 * ct + l16, k * KB + g * VE));
-                        x[ct] = W::mma(fa, rowf[k], x[ct]);
+                    for (int k = 0; k < KT; ++k) {
+                        colf = IC::across(now + L::COL, KB * k, 16 * ct, g, l16);
+#pragma unroll
+                        for (int term = 0; term < TERMS; ++term) x[ct] = W::mma(colf, rs[term][k], x[ct]);
                     }
                 }
+            }
+            passes = passes && cuts == 0;
+            base += n;
+            single = max(single - 1, 0);
         }
-        passes = passes && cuts == 0;
-        __syncthreads();
+        set = L::SET - set;
     }
     float *x_out = !MAIN ? p.spans + ((size_t)item * heads + head) * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
     if (!MAIN && tid == 0) p.spans[(size_t)job.items * heads * size + (size_t)item * heads + head] = passes ? 1.f : 0.f;
@@ -548,10 +542,20 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
     const float *passes = p.spans + (size_t)job.items * heads * size + (size_t)item * heads + head;
     const float w = (float)power((double)job.decay[head], job.span);
     float x = p.x_in ? p.x_in[((size_t)seg * heads + head) * size + e] : 0.f;
-    for (int i = 0; i + 1 < spans; ++i) {
-        const float f = passes[(size_t)i * heads] * w;
-        x = (f == 0.f ? 0.f : f * x) + at_span[(size_t)i * heads * size];
-        at_span[(size_t)i * heads * size] = x;
+    constexpr int AHEAD = 8;                              // spans whose numbers are under way together
+    for (int i = 0; i + 1 < spans; i += AHEAD) {
+        float f[AHEAD], v[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const size_t at = (size_t)min(i + k, spans - 2) * heads;
+            f[k] = passes[at] * w;
+            v[k] = at_span[at * size];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            x = (f[k] == 0.f ? 0.f : f[k] * x) + v[k];
+            if (i + k + 1 < spans) at_span[(size_t)(i + k) * heads * size] = x;
+        }
     }
 }
 
@@ -672,13 +676,13 @@ template <class T, int CP, int RP, bool MAIN, int TERMS>
 hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipStream_t s) {
     static size_t lds_set = 0;
     const auto kernel = decay_chunk_kernel<T, CP, RP, MAIN, TERMS>;
-    constexpr size_t lds = ChunkLds<T, CP, RP>::bytes(TERMS);
+    constexpr size_t lds = ChunkLds<T, CP, RP, MAIN>::BYTES;
     if (lds > 64 * 1024 && lds_set == 0) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
         lds_set = lds;
     }
-    launch(kernel, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP>::NT), lds, s, job);
+    launch(kernel, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP, MAIN>::NT), lds, s, job);
     return hipGetLastError();
 }
 // States are fp32 where they are handed out: a bfloat16 key with its decay then goes in as three terms, else as one.
@@ -722,13 +726,10 @@ int span_of(int heads, int n_segments, int n_tokens) {
 // Segments of up to so many tokens take the token-by-token kernel if the average is short.
 constexpr int BRIEF = 32;
 
-// Rows shorter than a load of the chunked kernels.
-constexpr int NARROW = 8;
-
-void plan(DecayJob &job, int heads, int key, int value) {
+void plan(DecayJob &job, int heads) {
     job.span = span_of(heads, job.n_segments, job.n_tokens);
     job.items = job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
-    job.brief = std::min(key, value) < NARROW ? INT32_MAX : job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
+    job.brief = job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
 }
 size_t spans_floats(const DecayJob &job, int heads, size_t size) {
     const int longest = job.seg_start ? job.n_tokens : job.len;
@@ -810,7 +811,7 @@ DecayJob job_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_
     j.seg_start = seg_start; j.starts = starts; j.n_segments = n_segments; j.n_tokens = n_tokens;
     j.len = n_tokens / n_segments;
     memcpy(j.decay, d->decay, sizeof(float) * d->n_heads);
-    plan(j, d->n_heads, d->key_dim, d->value_dim);
+    plan(j, d->n_heads);
     return j;
 }
 DecayPass pass_of(const ga3c_heads *row, const ga3c_heads *col, const ga3c_heads *by, const ga3c_heads *out, int rows, int cols, int turned, int back,
