@@ -432,7 +432,7 @@ int ga3c_get_desc(const ga3c_ctx *ctx, ga3c_net_desc *desc, int *max_predict_bat
  * type (dtype) in device memory: element (token, head, i) lies at
  * data[token * token_stride + head * head_stride + i], strides in elements, so
  * that they may be slices of one matrix.  Strides are not negative and a
- * token_stride is below 2^30; rows of an output do not overlap each other, nor
+ * token_stride is below 2^24; rows of an output do not overlap each other, nor
  * any input. */
 #define GA3C_F32  0
 #define GA3C_BF16 1

@@ -145,34 +145,51 @@ template <> struct Tile<bf16> {
 
 // One tensor's tile in LDS: C rows of D numbers, 16-byte pieces of a row in another order in each row, so that both ways of
 // reading reach all banks: the same piece of sixteen rows, and (16 bits) two neighbouring pieces of rows 0-3, 8-11, 16-19, 24-27,
-// (32 bits) four pieces of every fourth row.
+// (32 bits) four pieces of every fourth row.  The order is an exclusive or, so a lane's place in one step of a contraction gives
+// the others with one instruction each: `start` is the lane's, the rest is the same for all lanes.
 template <class T, int D>
 struct Image {
     typedef Tile<T> W;
-    static constexpr int PIECES = D * (int)sizeof(T) / 16, BYTES = W::C * PIECES * 16;
+    static constexpr int PIECES = D * (int)sizeof(T) / 16, ROW = 16 * PIECES, BYTES = W::C * ROW;
     __device__ static int order(int row) {
         if (sizeof(T) == 4) return row & 15;
         if (PIECES >= 16) return (row >> 2 & 1) | (row & 3) << 1 | (row & 8);
         return (row >> 2 & 1) | (row & 2) | (row >> 1 & 4);
     }
-    __device__ static int place(int row, int piece) { return (row * PIECES + (piece ^ order(row))) * 16; }
-    // numbers k .. k + VE - 1 of a row
-    __device__ static typename W::Frag along(const char *at, int row, int k) { return *(const typename W::Frag *)(at + place(row, k / W::VE)); }
-    // (bfloat16) four numbers from an even quad on
-    __device__ static bf16x4 four(const char *at, int row, int k) { return *(const bf16x4 *)(at + place(row, k / 8) + k % 8 * 2); }
-    // column first + l16 of rows j + VE g .. + VE - 1, as the lanes of an operand hold them
-    __device__ static typename W::Frag across(const char *at, int j, int first, int g, int l16) {
+    // numbers KB step + VE g .. + VE - 1 of row 16 tile + l16
+    __device__ static int along_start(int g, int l16) { return l16 * ROW + (g ^ order(l16)) * 16; }
+    __device__ static typename W::Frag along(const char *at, int start, int tile, int step) {
+        return *(const typename W::Frag *)(at + (start ^ step * 64) + tile * 16 * ROW);
+    }
+    // (bfloat16) numbers 32 step + 4 g .. + 3 and as many from 16 further on
+    __device__ static int fours_start(int g, int l16) { return l16 * ROW + (g / 2 ^ order(l16)) * 16 + g % 2 * 8; }
+    __device__ static bf16x8 fours(const char *at, int start, int tile, int step) {
+        const bf16x4 a = *(const bf16x4 *)(at + (start ^ step * 64) + tile * 16 * ROW), b = *(const bf16x4 *)(at + (start ^ (step * 64 + 32)) + tile * 16 * ROW);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // column 16 tile + l16 of rows KB step + VE g .. + VE - 1, as the lanes of an operand hold them
+    struct Across { int at[sizeof(T) == 4 ? 4 : 1]; };
+    __device__ static Across across_start(int g, int l16) {
+        Across r;
+        if constexpr (sizeof(T) == 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.at[e] = (4 * g + e) * ROW + (l16 / 4 ^ (4 * g + e)) * 16 + l16 % 4 * 4;
+        else {
+            // lanes 4 t .. 4 t + 3 give the places of a row's four quads, and lane i takes column i of the four rows
+            const int row = 8 * g + l16 / 4;
+            r.at[0] = row * ROW + (l16 % 4 / 2 ^ order(row)) * 16 + l16 % 2 * 8;
+        }
+        return r;
+    }
+    __device__ static typename W::Frag across(const char *at, const Across &start, int tile, int step) {
         typename W::Frag f;
         if constexpr (sizeof(T) == 4) {
-            const int c = first + l16;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = *(const float *)(at + place(j + 4 * g + e, c / 4) + c % 4 * 4);
+            for (int e = 0; e < 4; ++e) f[e] = *(const float *)(at + (start.at[e] ^ tile * 64) + step * 16 * ROW);
         } else {
-            // lanes 4 t .. 4 t + 3 give the places of a row's four quads, and lane i takes column i of the four rows
-            const int row = j + 8 * g + l16 / 4, k = first + 4 * (l16 % 4);
             typedef __attribute__((address_space(3))) s16x4 *Lds;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + place(row, k / 8) + k % 8 * 2));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + place(row + 4, k / 8) + k % 8 * 2));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + (start.at[0] ^ tile * 32) + step * 32 * ROW));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + (start.at[0] ^ (tile * 32 + 16)) + (step * 32 + 4) * ROW));
             f = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         return f;
@@ -231,10 +248,18 @@ __device__ inline bool find_item(const DecayJob &p, int item, int &seg, int &spa
 // Pieces of rows that are not there.
 __device__ const uint4 decay_nothing[1] = {{0, 0, 0, 0}};
 
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ inline const void *uniform(const void *p) {
+    const uint64_t u = (uint64_t)p;
+    return (const void *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
 // 16 bytes per lane to lds + 16 * lane; lds is the same for the whole wavefront.  The caller waits for vmcnt itself: the compiler,
 // which would wait for every such load in front of the next LDS read, does not see it.
 __device__ inline void piece_to_lds(const void *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+}
+__device__ inline void piece_to_lds(const void *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // VE elements of a row from element `i` on, zero behind its `dim` elements; rows begin anywhere.
 template <class T>
@@ -251,24 +276,35 @@ template <class T>
 __device__ inline bool whole_pieces(const DecayView &v, int dim) {
     return (uintptr_t)v.data % 16 == 0 && ((v.token | v.head | dim) % Tile<T>::VE) == 0;
 }
-// The tile of one tensor: positions base .. base + n - 1 of the span, zeros behind them.
+// The tile of one tensor: n positions of the span, `lowest` the first of their tokens in memory, zeros behind them.
+// off: of this thread's piece in a whole tile (tile_offset).
 template <class T, int D, int NT>
-__device__ inline void stage(const DecayView &v, int dim, bool whole, int lowest, int n, bool back, int head, char *to, int wave) {
+__device__ inline uint32_t tile_offset(const DecayView &v, bool back, int tid) {
     typedef Image<T, D> I;
-    const int lane = fresh_lane();
-    const char *rows = (const char *)at<T>(v, lowest, head);         // the tile's first token in memory
+    const int pos = tid / I::PIECES, piece = tid % I::PIECES ^ I::order(pos);
+    return (uint32_t)(back ? Tile<T>::C - 1 - pos : pos) * (uint32_t)v.token * (uint32_t)sizeof(T) + piece * 16;
+}
+template <class T, int D, int NT>
+__device__ inline void stage(const DecayView &v, int dim, bool whole, uint32_t off, int lowest, int n, bool back, int head, char *to, int wave) {
+    typedef Image<T, D> I;
+    constexpr int ALL = I::BYTES / 16, STEP = NT / I::PIECES;        // positions from one piece of a thread to the next
+    static_assert(ALL % 64 == 0 && STEP % 16 == 0, "whole wavefronts, and a thread's rows in one order");
+    const char *rows = (const char *)at<T>(v, lowest, head);
     const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
-    constexpr int ALL = I::BYTES / 16;
-    static_assert(ALL % 64 == 0, "whole wavefronts");
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + wave * 1024);
+    const bool full = whole && n == Tile<T>::C && dim == D;
 #pragma unroll
     for (int k = 0; k < (ALL + NT - 1) / NT; ++k) {
-        const int first = 64 * wave + NT * k;
-        if (ALL % NT && first >= ALL) break;
-        const int s = first + lane, pos = s / I::PIECES, piece = (s % I::PIECES) ^ I::order(pos), i = piece * Tile<T>::VE;
+        if (ALL % NT && 64 * wave + NT * k >= ALL) break;
+        if (full) {
+            const int64_t further = (int64_t)(STEP * k) * step;
+            piece_to_lds(uniform(rows + (back ? -further : further)), off, lds + NT * 16 * k);
+            continue;
+        }
+        const int s = 64 * wave + NT * k + fresh_lane(), pos = s / I::PIECES, piece = (s % I::PIECES) ^ I::order(pos), i = piece * Tile<T>::VE;
         const char *row = rows + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * step;
         if (whole)
-            piece_to_lds(pos < n && i < dim ? (const void *)(row + piece * 16) : (const void *)decay_nothing,
-                         __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + first * 16));
+            piece_to_lds(pos < n && i < dim ? (const void *)(row + piece * 16) : (const void *)decay_nothing, lds + NT * 16 * k);
         else {
             uint4 u{0, 0, 0, 0};
             if (pos < n && i < dim) u = loose_piece((const T *)row, i, dim);
@@ -320,13 +356,16 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     const bool back = p.back, turned = p.turned, last = to == whole;
     const int rows = p.rows, cols = p.cols, a = back ? 0 : 1;
     const float d = job.decay[head];
+    const bool fades = (float)power((double)d, C) == 0.f;           // some factors of a tile are zero
     const bool pieces = whole_pieces<T>(p.col, cols) && whole_pieces<T>(p.row, rows) && whole_pieces<T>(p.by, cols);
+    const uint32_t col_off = tile_offset<T, CP, NT>(p.col, back, tid), row_off = tile_offset<T, RP, NT>(p.row, back, tid),
+                   by_off = MAIN ? tile_offset<T, CP, NT>(p.by, back, tid) : 0;
     int flag = 0;
     auto fetch = [&](int base, int n, char *set) {
         const int lowest = back ? end - base - n : first + base;
-        stage<T, CP, NT>(p.col, cols, pieces, lowest, n, back, head, set + L::COL, wave);
-        stage<T, RP, NT>(p.row, rows, pieces, lowest, n, back, head, set + L::ROW, wave);
-        if (MAIN) stage<T, CP, NT>(p.by, cols, pieces, lowest, n, back, head, set + L::BY, wave);
+        stage<T, CP, NT>(p.col, cols, pieces, col_off, lowest, n, back, head, set + L::COL, wave);
+        stage<T, RP, NT>(p.row, rows, pieces, row_off, lowest, n, back, head, set + L::ROW, wave);
+        if (MAIN) stage<T, CP, NT>(p.by, cols, pieces, by_off, lowest, n, back, head, set + L::BY, wave);
         if (job.starts) {
             // backward, the cut lies between a token and the one behind it
             const int pos = min(lane, n - 1), t = lowest + (back ? n - pos : pos);
@@ -364,11 +403,15 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     const bool vec_out = (uintptr_t)p.out.data % (4 * sizeof(T)) == 0 && ((p.out.token | p.out.head | rows) % 4) == 0;
     bool passes = true;                                             // whether the state in front of the span reaches its end
     const bool mine = RP / 16 == WAVES || wave < RP / 16;
+    const int along = IC::along_start(g, l16), fours = IC::fours_start(g, l16);
+    const auto row_across = IR::across_start(g, l16);
+    const auto col_across = IC::across_start(g, l16);
     __syncthreads();                                                // pw
     while (base < to) {
         const int n = single ? 1 : min(C, to - base);
         const uint64_t cuts = job.starts ? __ballot(lane < n && flag && !(back && base + lane == 0)) : 0;
         const int cut = cuts ? 63 - __clzll(cuts) : -1;             // the tile's last start
+        const bool whole_tile = cuts == 0 && !fades;                // every position sees the state, and it stays
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const char *const now = lds + set;
@@ -381,7 +424,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
         if (mine)
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                rowf[k] = IR::across(now + L::ROW, KB * k, 16 * wave, g, l16);
+                rowf[k] = IR::across(now + L::ROW, row_across, wave, k);
                 wrong = wrong || not_finite<T>(__builtin_bit_cast(uint4, rowf[k]));
             }
         if (cuts)
@@ -398,7 +441,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                 f32x4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < CP / KB; ++c)
-                    s = W::mma(IC::along(now + L::COL, 16 * jt + l16, c * KB + g * VE), IC::along(now + L::BY, 16 * it + l16, c * KB + g * VE), s);
+                    s = W::mma(IC::along(now + L::COL, along, jt, c), IC::along(now + L::BY, along, it, c), s);
                 const int i = 16 * it + l16;
                 const uint64_t before = cuts & (~0ull >> (63 - i));
                 const int fresh = before ? 63 - __clzll(before) : -1;
@@ -421,7 +464,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     __builtin_amdgcn_sched_barrier(0);      // loads of all steps at once would not fit the registers
                     if constexpr (KB == 16) {
 #pragma unroll
-                        for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], IC::along(now + L::BY, 16 * it + l16, KB * c + 4 * g), acc[it]);
+                        for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], IC::along(now + L::BY, along, it, c), acc[it]);
                     } else {       // two terms of the state, 16 bits: one alone doubles the error of the result's own rounding
                         const f32x4 x0 = x[2 * c % CT], x1 = x[(2 * c + 1) % CT];
                         const bf16x4 h0 = W::quad(x0), h1 = W::quad(x1);
@@ -429,8 +472,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                         const bf16x8 h = __builtin_shufflevector(h0, h1, 0, 1, 2, 3, 4, 5, 6, 7), l = __builtin_shufflevector(l0, l1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
                         for (int it = 0; it < IT; ++it) {
-                            const bf16x4 b0 = IC::four(now + L::BY, 16 * it + l16, KB * c + 4 * g), b1 = IC::four(now + L::BY, 16 * it + l16, KB * c + 16 + 4 * g);
-                            const bf16x8 fb = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
+                            const bf16x8 fb = IC::fours(now + L::BY, fours, it, c);
                             acc[it] = W::mma(h, fb, acc[it]);
                             acc[it] = W::mma(l, fb, acc[it]);
                         }
@@ -439,14 +481,16 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
                     const int i = 16 * it + l16;
-                    acc[it] = scaled(acc[it], cuts & (~0ull >> (63 - i)) ? 0.f : pw[min(i + a, C)]);
+                    const float w = pw[min(i + a, C)];
+                    if (whole_tile) acc[it] = acc[it] * w;
+                    else acc[it] = scaled(acc[it], cuts & (~0ull >> (63 - i)) ? 0.f : w);
                 }
             }
         }
         __syncthreads();
         // A product with zero does not hide a number that is not finite from the positions that must not see it: one position at
         // a time then.
-        if (!single && n > 1 && *odd) {
+        if (!single && n > 1 && __builtin_amdgcn_readfirstlane(*odd)) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (tid == 0) *odd = 0;
@@ -465,7 +509,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                             acc[it] = W::mma(rowf[k], *(const typename W::Frag *)(P + (16 * it + l16) * L::JB + k * KB + g * VE), acc[it]);
                         const int pos = 16 * it + l16, o = 16 * wave + 4 * g;
                         const typename W::Quad w = W::quad(acc[it] * p.out_scale);
-                        T *out = (T *)(out_tile + (uint64_t)(uint32_t)(back ? n - 1 - pos : pos) * out_step);
+                        T *out = (T *)(out_tile + (uint32_t)(back ? n - 1 - pos : pos) * out_step);
                         if (pos < n && vec_out) {
                             if (o < rows) *(typename W::Quad *)(out + o) = w;
                         } else if (pos < n) {
@@ -491,13 +535,19 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                         }
                 }
                 const float carry = cuts ? 0.f : pw[n];
+                if (whole_tile) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) x[ct] = x[ct] * carry;
+                } else {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) x[ct] = scaled(x[ct], carry);
+                }
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-                    x[ct] = scaled(x[ct], carry);
 #pragma unroll
                     for (int k = 0; k < KT; ++k) {
-                        colf = IC::across(now + L::COL, KB * k, 16 * ct, g, l16);
+                        colf = IC::across(now + L::COL, col_across, ct, k);
 #pragma unroll
                         for (int term = 0; term < TERMS; ++term) x[ct] = W::mma(colf, rs[term][k], x[ct]);
                     }
@@ -773,18 +823,18 @@ bool apart(const ga3c_heads &v, int n, int heads, int dim) {
     if (t < dim || h < dim) return false;
     return n <= 1 || heads <= 1 || t >= h * (heads - 1) + dim || h >= t * (n - 1) + dim;
 }
-constexpr int64_t MAX_STRIDE = 1 << 30;      // a step in bytes is a 32-bit number in the kernels
+constexpr int64_t MAX_STRIDE = 1 << 24;      // the 64 positions of a tile are 32-bit numbers of bytes apart
 int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *out, const int *out_dims, int n_out, int n, int heads, size_t size, const char *who) {
     for (int i = 0; i < n_in; ++i) {
         if (!in[i] || !in[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)in[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
         if (in[i]->token_stride < 0 || in[i]->head_stride < 0) return call_fail(GA3C_EINVAL, "%s: negative stride", who);
-        if (in[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^30 or more", who);
+        if (in[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
     }
     for (int i = 0; i < n_out; ++i) {
         if (!out[i] || !out[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)out[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
-        if (out[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^30 or more", who);
+        if (out[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
         if (!apart(*out[i], n, heads, out_dims[i])) return call_fail(GA3C_EINVAL, "%s: strides make rows of an output overlap", who);
         for (int k = 0; k < n_in; ++k)
             if (out[i]->data == in[k]->data) return call_fail(GA3C_EINVAL, "%s: an output is one of the inputs", who);
