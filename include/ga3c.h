@@ -459,6 +459,7 @@ typedef struct {
  *   S = 0 where starts[t] != 0;  S = decay S + v_t k_t^T;  out_t = scale S q_t
  * and state_out receives S behind the segment's last token.
  *   q, k          [n_tokens][n_heads][key_dim];  v, out [n_tokens][n_heads][value_dim]
+ *                 (n_segments <= 2^24)
  *   seg_start_dev i32 [n_segments+1] as for ga3c_train_step_ragged (checked no
  *                 more than there: a bad table gives wrong results, no access
  *                 outside the arrays), or NULL: segments of equal length

@@ -29,16 +29,50 @@ __device__ inline void segment_tokens(const DecayJob &p, int seg, int &first, in
 template <class T>
 __device__ inline const T *at(const DecayView &v, int token, int head) { return (const T *)v.data + token * v.token + head * v.head; }
 
-// Token by token.  A block takes ROWS rows of one segment's state in one head: LPR lanes share a row, four (or twice four) columns
-// each, and a lane has DR_RPL rows.
-constexpr int DR_RPL = 4;
-template <class T, int LPR, int CV>
-__global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job, int slices) {
-    constexpr int RW = 64 / LPR, ROWS = 4 * RW * DR_RPL;
-    const DecayPass &p = job.pass[blockIdx.z / slices];
-    const int seg = blockIdx.x, head = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int heads = gridDim.y, c0 = lane % LPR * 4, r0 = blockIdx.z % slices * ROWS + wave * RW * DR_RPL + lane / LPR;
-    const float d = job.decay[head];
+// ----------------------------------------------------------------- token by token --
+//
+// A wavefront takes RPL * 64 / LPR rows of one segment's state in one head: LPR lanes share a row, four columns each (or twice
+// four), and a lane has RPL rows.  Bound by the latency of memory: the tokens come eight (or four) at a time, so that those of a
+// segment of an update are on their way together.
+template <int RPL, int CV>
+struct Rows {
+    float4 x[RPL][CV];
+    // one token: keep * x + row col^T, read out by `by`; the sums over a row are the same in its LPR lanes
+    template <int LPR>
+    __device__ void take(float keep, const float (&row)[RPL], const float4 (&col)[CV], const float4 (&by)[CV], float (&sum)[RPL]) {
+#pragma unroll
+        for (int i = 0; i < RPL; ++i) {
+            sum[i] = 0.f;
+#pragma unroll
+            for (int v = 0; v < CV; ++v) {
+                float4 &y = x[i][v];
+                if (keep == 0.f) y = float4{0.f, 0.f, 0.f, 0.f};        // whatever was in it
+                y.x = keep * y.x + row[i] * col[v].x; y.y = keep * y.y + row[i] * col[v].y;
+                y.z = keep * y.z + row[i] * col[v].z; y.w = keep * y.w + row[i] * col[v].w;
+                sum[i] += y.x * by[v].x + y.y * by[v].y + y.z * by[v].z + y.w * by[v].w;
+            }
+#pragma unroll
+            for (int m = LPR / 2; m > 0; m /= 2) sum[i] += __shfl_xor(sum[i], m);
+        }
+    }
+    __device__ void fade(float f) {
+#pragma unroll
+        for (int i = 0; i < RPL; ++i)
+#pragma unroll
+            for (int v = 0; v < CV; ++v) {
+                float4 &y = x[i][v];
+                y = f == 0.f ? float4{0.f, 0.f, 0.f, 0.f} : float4{f * y.x, f * y.y, f * y.z, f * y.w};
+            }
+    }
+};
+
+template <class T, int LPR, int CV, int RPL>
+__global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job, int slabs) {
+    constexpr int RW = 64 / LPR;
+    const DecayPass &p = job.pass[blockIdx.z];
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int seg = unit / slabs, head = blockIdx.y, heads = gridDim.y, c0 = lane % LPR * 4, r0 = unit % slabs * RW * RPL + lane / LPR;
+    if (seg >= job.n_segments) return;
     int first, end;
     segment_tokens(job, seg, first, end);
     if (end - first > job.brief) return;
@@ -46,63 +80,82 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job
                     ((p.col.token | p.col.head | p.by.token | p.by.head) % 4 == 0);
     const size_t state = ((size_t)seg * heads + head) * p.rows * p.cols;
     const bool turned = p.turned, back = p.back;
-    float4 x[DR_RPL][CV];
+    const int row_step = turned ? 1 : p.cols, col_step = turned ? p.rows : 1;
+    const float d = job.decay[head];
+    Rows<RPL, CV> s;
+    const bool quads = !turned && p.cols % 4 == 0 && ((uintptr_t)p.x_in | (uintptr_t)p.x_out) % 16 == 0;
 #pragma unroll
-    for (int i = 0; i < DR_RPL; ++i)
+    for (int i = 0; i < RPL; ++i)
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
             const int r = r0 + i * RW, c = c0 + v * 4 * LPR;
-            float e[4] = {0.f, 0.f, 0.f, 0.f};
-            if (p.x_in && r < p.rows)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < p.cols) e[k] = p.x_in[state + (turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)];
-            x[i][v] = float4{e[0], e[1], e[2], e[3]};
-        }
-    for (int n = first; n < end; ++n) {
-        const int t = back ? end - 1 - (n - first) : n;
-        const bool start = job.starts && job.starts[t];
-        const float keep = back ? 1.f : start ? 0.f : d;
-        float4 col[CV], by[CV];
-#pragma unroll
-        for (int v = 0; v < CV; ++v) {
-            const int c = c0 + v * 4 * LPR;
-            col[v] = load4(at<T>(p.col, t, head) + c, p.cols - c, vec);
-            by[v] = load4(at<T>(p.by, t, head) + c, p.cols - c, vec);
-        }
-#pragma unroll
-        for (int i = 0; i < DR_RPL; ++i) {
-            const int r = r0 + i * RW;
-            const float row = r < p.rows ? p.col_scale * to_f32(at<T>(p.row, t, head)[r]) : 0.f;
-            float sum = 0.f;
-#pragma unroll
-            for (int v = 0; v < CV; ++v) {
-                float4 &y = x[i][v];
-                if (keep == 0.f) y = float4{0.f, 0.f, 0.f, 0.f};        // whatever was in it
-                y.x = keep * y.x + row * col[v].x; y.y = keep * y.y + row * col[v].y;
-                y.z = keep * y.z + row * col[v].z; y.w = keep * y.w + row * col[v].w;
-                sum += y.x * by[v].x + y.y * by[v].y + y.z * by[v].z + y.w * by[v].w;
-                if (back) {
-                    const float f = start ? 0.f : d;
-                    y = f == 0.f ? float4{0.f, 0.f, 0.f, 0.f} : float4{f * y.x, f * y.y, f * y.z, f * y.w};
+            float4 e{0.f, 0.f, 0.f, 0.f};
+            if (p.x_in && r < p.rows) {
+                const float *x = p.x_in + state + (uint32_t)(r * row_step + c * col_step);
+                if (quads) {
+                    if (c < p.cols) e = load4(x, 4, true);
+                } else {
+                    if (c < p.cols) e.x = x[0];
+                    if (c + 1 < p.cols) e.y = x[col_step];
+                    if (c + 2 < p.cols) e.z = x[2 * col_step];
+                    if (c + 3 < p.cols) e.w = x[3 * col_step];
                 }
             }
+            s.x[i][v] = e;
+        }
+    constexpr int TOGETHER = CV == 1 ? 8 : 4;
+    for (int n = first; n < end; n += TOGETHER) {
+        float4 col[TOGETHER][CV], by[TOGETHER][CV];
+        float row[TOGETHER][RPL];
+        int starts = 0;
 #pragma unroll
-            for (int m = LPR / 2; m > 0; m /= 2) sum += __shfl_xor(sum, m);
-            if (lane % LPR == 0 && r < p.rows) ((T *)p.out.data)[t * p.out.token + head * p.out.head + r] = from_f32<T>(p.out_scale * sum);
+        for (int k = 0; k < TOGETHER; ++k) {
+            const int pos = min(n + k, end - 1), t = back ? end - 1 - (pos - first) : pos;
+            const T *pc = at<T>(p.col, t, head), *pb = at<T>(p.by, t, head), *pr = at<T>(p.row, t, head);
+#pragma unroll
+            for (int v = 0; v < CV; ++v) {
+                const int c = c0 + v * 4 * LPR;
+                col[k][v] = load4(pc + c, p.cols - c, vec);
+                by[k][v] = load4(pb + c, p.cols - c, vec);
+            }
+#pragma unroll
+            for (int i = 0; i < RPL; ++i) row[k][i] = r0 + i * RW < p.rows ? to_f32(pr[r0 + i * RW]) : 0.f;
+            if (job.starts) starts |= (job.starts[t] != 0) << k;
+        }
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) {
+            if (n + k >= end) break;
+            const int t = back ? end - 1 - (n + k - first) : n + k;
+            const bool start = starts >> k & 1;
+            float sum[RPL];
+#pragma unroll
+            for (int i = 0; i < RPL; ++i) row[k][i] *= p.col_scale;
+            s.template take<LPR>(back ? 1.f : start ? 0.f : d, row[k], col[k], by[k], sum);
+            if (back) s.fade(start ? 0.f : d);
+            T *out = (T *)p.out.data + t * p.out.token + head * p.out.head;
+            if (lane % LPR == 0)
+#pragma unroll
+                for (int i = 0; i < RPL; ++i)
+                    if (r0 + i * RW < p.rows) out[r0 + i * RW] = from_f32<T>(p.out_scale * sum[i]);
         }
     }
     if (!p.x_out) return;
 #pragma unroll
-    for (int i = 0; i < DR_RPL; ++i)
+    for (int i = 0; i < RPL; ++i)
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
             const int r = r0 + i * RW, c = c0 + v * 4 * LPR;
-            const float e[4] = {x[i][v].x, x[i][v].y, x[i][v].z, x[i][v].w};
-            if (r < p.rows)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < p.cols) p.x_out[state + (turned ? (size_t)(c + k) * p.rows + r : (size_t)r * p.cols + c + k)] = e[k];
+            if (r >= p.rows) continue;
+            const float4 e = s.x[i][v];
+            float *x = p.x_out + state + (uint32_t)(r * row_step + c * col_step);
+            if (quads) {
+                if (c < p.cols) *(float4 *)x = e;
+            } else {
+                if (c < p.cols) x[0] = e.x;
+                if (c + 1 < p.cols) x[col_step] = e.y;
+                if (c + 2 < p.cols) x[2 * col_step] = e.z;
+                if (c + 3 < p.cols) x[3 * col_step] = e.w;
+            }
         }
 }
 
@@ -225,23 +278,31 @@ __device__ inline double power(double d, int e) {
 }
 
 // Which segment and which span of it the item is; false: none.  A wavefront looks at 64 places of the table at a time.
+// Where short segments are left to the other kernel there are no spans, and item i is the segment that token i * (brief + 1) lies
+// in, if no smaller one does: a segment that is longer than `brief` holds one of these.
 __device__ inline bool find_item(const DecayJob &p, int item, int &seg, int &span) {
     if (!p.seg_start) {
         const int each = p.len / p.span + 1;
         seg = item / each; span = item % each;
         return seg < p.n_segments;
     }
-    const int lane = threadIdx.x % 64;
+    const int lane = threadIdx.x % 64, place = p.brief >= 0 ? item * (p.brief + 1) : item;
     int lo = 0, hi = p.n_segments;                         // the last segment whose items begin at or before this one
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-        const bool before = i < hi && min(max(p.seg_start[min(i, p.n_segments)], 0), p.n_tokens) / p.span + i <= item;
+        const int begins = min(max(p.seg_start[min(i, p.n_segments)], 0), p.n_tokens);
+        const bool before = i < hi && (p.brief >= 0 ? begins : begins / p.span + i) <= place;
         const int k = max(1, __popcll(__ballot(before)));
         lo += (k - 1) * step;
         hi = min(hi, lo + step);
     }
     seg = lo;
-    span = item - (min(max(p.seg_start[seg], 0), p.n_tokens) / p.span + seg);
+    const int begins = min(max(p.seg_start[seg], 0), p.n_tokens);
+    if (p.brief >= 0) {          // the item is the first of its segment
+        span = 0;
+        return begins <= place && place - begins <= p.brief;
+    }
+    span = item - (begins / p.span + seg);
     return span >= 0;
 }
 
@@ -544,7 +605,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                 }
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                    if (MAIN && ct % 4 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int k = 0; k < KT; ++k) {
                         colf = IC::across(now + L::COL, col_across, ct, k);
@@ -612,6 +673,7 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
 // One token of each agent.  The state of entry i is row slots[i] of the states (i without slots), read, advanced and written back;
 // a slot outside them stands for a state of zeros that is not kept.  Entries that name one slot are consecutive tokens of it, in
 // the order of their numbers: the first of them takes the others along, so that nobody else touches the slot.
+// Bound by memory: a state is read and written once.
 struct DecayStep {
     DecayView q, k, v, out;
     int key, value;
@@ -622,78 +684,109 @@ struct DecayStep {
     float scale;
     float decay[GA3C_MAX_HEADS];
 };
-// The first entry from `from` on with this slot, n if there is none; the same in all threads of the block.
-__device__ inline int next_of_slot(const DecayStep &p, int slot, int from, int to, int *lowest) {
-    __syncthreads();
-    if (threadIdx.x == 0) *lowest = p.n;
-    __syncthreads();
-    int mine = p.n;
-    for (int j = from + threadIdx.x; j < to; j += 256)
-        if (p.slots[j] == slot) { mine = j; break; }
-    if (mine < p.n) atomicMin(lowest, mine);
-    __syncthreads();
-    return *lowest;
+// The first entry behind `entry` with this slot, p.n if there is none, -1 if there is one in front of it (looked for only where
+// `first`); the same in all lanes of the wavefront.
+__device__ inline int next_of_slot(const DecayStep &p, int slot, int entry, bool first) {
+    const int lane = threadIdx.x % 64;
+    for (int j = first ? 0 : entry + 1; j < p.n; j += 512) {
+        bool is[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int at = j + 64 * k + lane;
+            is[k] = p.slots[min(at, p.n - 1)] == slot && at < p.n && at != entry;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint64_t m = __ballot(is[k]);
+            if (m) {
+                const int found = j + 64 * k + __ffsll((unsigned long long)m) - 1;
+                return found < entry ? -1 : found;
+            }
+        }
+    }
+    return p.n;
 }
 
-template <class T, int LPR, int CV>
-__global__ __launch_bounds__(256) void decay_step_kernel(const DecayStep p, int vec) {
-    constexpr int RW = 64 / LPR, ROWS = 4 * RW * DR_RPL;
-    __shared__ int lowest;
-    const int head = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64, heads = gridDim.y;
-    const int c0 = lane % LPR * 4, r0 = blockIdx.z * ROWS + wave * RW * DR_RPL + lane / LPR;
-    const int slot = p.slots ? p.slots[blockIdx.x] : (int)blockIdx.x;
-    const bool kept = slot >= 0 && slot < p.n_slots;
-    if (p.slots && kept && next_of_slot(p, slot, 0, blockIdx.x, &lowest) < p.n) return;
+// Four numbers that the caches need not keep.
+typedef float f32x4_once __attribute__((ext_vector_type(4)));
+__device__ inline float4 load_once(const float *p) {
+    const f32x4_once v = __builtin_nontemporal_load((const f32x4_once *)p);
+    return float4{v.x, v.y, v.z, v.w};
+}
+__device__ inline void store_once(float *p, float4 v) { __builtin_nontemporal_store(f32x4_once{v.x, v.y, v.z, v.w}, (f32x4_once *)p); }
+
+// STREAM: the states of a call are more than the caches hold, and may be moved four numbers at a time.
+template <class T, int LPR, int CV, int RPL, bool STREAM>
+__global__ __launch_bounds__(256) void decay_step_kernel(const DecayStep p, int slabs, int vec) {
+    constexpr int RW = 64 / LPR;
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int entry = unit / slabs, head = blockIdx.y, heads = gridDim.y, c0 = lane % LPR * 4, r0 = unit % slabs * RW * RPL + lane / LPR;
+    if (entry >= p.n) return;
+    const int slot = p.slots ? __builtin_amdgcn_readfirstlane(p.slots[entry]) : entry;
+    const bool kept = slot >= 0 && slot < p.n_slots, shared = p.slots && kept;
     const float d = p.decay[head];
     float *state = p.states + ((size_t)(kept ? slot : 0) * heads + head) * p.value * p.key;
-    float4 x[DR_RPL][CV];
+    const bool quads = p.key % 4 == 0 && (uintptr_t)p.states % 16 == 0;
+    Rows<RPL, CV> s;
 #pragma unroll
-    for (int i = 0; i < DR_RPL; ++i)
+    for (int i = 0; i < RPL; ++i)
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
             const int r = r0 + i * RW, c = c0 + v * 4 * LPR;
-            x[i][v] = load4(state + (size_t)r * p.key + c, kept && r < p.value ? p.key - c : 0, p.key % 4 == 0 && vec);
+            const float *x = state + (uint32_t)(r * p.key + c);
+            if (STREAM) s.x[i][v] = r < p.value && c < p.key && kept ? load_once(x) : float4{0.f, 0.f, 0.f, 0.f};
+            else s.x[i][v] = load4(x, kept && r < p.value ? p.key - c : 0, quads);
         }
-    for (int t = blockIdx.x; t < p.n; t = p.slots && kept ? next_of_slot(p, slot, t + 1, p.n, &lowest) : p.n) {
-        const float keep = p.starts && p.starts[t] ? 0.f : d;
-        float4 col[CV], by[CV];
+    float4 col[CV], by[CV];
+    float row[RPL], sum[RPL];
+    int start;
+    auto fetch = [&](int t) {
+        const T *q = at<T>(p.q, t, head), *k = at<T>(p.k, t, head), *w = at<T>(p.v, t, head);
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
             const int c = c0 + v * 4 * LPR;
-            col[v] = load4(at<T>(p.k, t, head) + c, p.key - c, vec);
-            by[v] = load4(at<T>(p.q, t, head) + c, p.key - c, vec);
+            col[v] = load4(k + c, p.key - c, vec);
+            by[v] = load4(q + c, p.key - c, vec);
         }
 #pragma unroll
-        for (int i = 0; i < DR_RPL; ++i) {
-            const int r = r0 + i * RW;
-            const float row = r < p.value ? to_f32(at<T>(p.v, t, head)[r]) : 0.f;
-            float sum = 0.f;
+        for (int i = 0; i < RPL; ++i) row[i] = r0 + i * RW < p.value ? to_f32(w[r0 + i * RW]) : 0.f;
+        start = p.starts ? p.starts[t] : 0;
+    };
+    fetch(entry);
+    // (all of that is on its way meanwhile)
+    int next = shared ? next_of_slot(p, slot, entry, true) : p.n;
+    if (next < 0) return;
+    for (int t = entry;;) {
+        s.template take<LPR>(start ? 0.f : d, row, col, by, sum);
+        T *out = (T *)p.out.data + t * p.out.token + head * p.out.head;
+        if (lane % LPR == 0)
 #pragma unroll
-            for (int v = 0; v < CV; ++v) {
-                float4 &y = x[i][v];
-                if (keep == 0.f) y = float4{0.f, 0.f, 0.f, 0.f};
-                y.x = keep * y.x + row * col[v].x; y.y = keep * y.y + row * col[v].y;
-                y.z = keep * y.z + row * col[v].z; y.w = keep * y.w + row * col[v].w;
-                sum += y.x * by[v].x + y.y * by[v].y + y.z * by[v].z + y.w * by[v].w;
-            }
-#pragma unroll
-            for (int m = LPR / 2; m > 0; m /= 2) sum += __shfl_xor(sum, m);
-            if (lane % LPR == 0 && r < p.value) ((T *)p.out.data)[t * p.out.token + head * p.out.head + r] = from_f32<T>(p.scale * sum);
-        }
+            for (int i = 0; i < RPL; ++i)
+                if (r0 + i * RW < p.value) out[r0 + i * RW] = from_f32<T>(p.scale * sum[i]);
+        if (next >= p.n) break;
+        t = next;
+        fetch(t);
+        next = next_of_slot(p, slot, t, false);
     }
     if (!kept) return;
 #pragma unroll
-    for (int i = 0; i < DR_RPL; ++i)
+    for (int i = 0; i < RPL; ++i)
 #pragma unroll
         for (int v = 0; v < CV; ++v) {
             const int r = r0 + i * RW, c = c0 + v * 4 * LPR;
             if (r >= p.value) continue;
-            float *to = state + (size_t)r * p.key + c;
-            if (p.key % 4 == 0 && vec && c + 4 <= p.key) { *(float4 *)to = x[i][v]; continue; }
-            const float e[4] = {x[i][v].x, x[i][v].y, x[i][v].z, x[i][v].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < p.key) to[k] = e[k];
+            const float4 e = s.x[i][v];
+            float *x = state + (uint32_t)(r * p.key + c);
+            if (STREAM) {
+                if (c < p.key) store_once(x, e);
+            } else if (quads) {
+                if (c < p.key) *(float4 *)x = e;
+            } else {
+                if (c < p.key) x[0] = e.x;
+                if (c + 1 < p.key) x[1] = e.y;
+                if (c + 2 < p.key) x[2] = e.z;
+                if (c + 3 < p.key) x[3] = e.w;
+            }
         }
 }
 
@@ -703,21 +796,32 @@ __global__ __launch_bounds__(256) void decay_step_kernel(const DecayStep p, int 
 template <class T>
 bool rows_of_four(const DecayView &v) { return (uintptr_t)v.data % (4 * sizeof(T)) == 0 && v.token % 4 == 0 && v.head % 4 == 0; }
 
+// go(LPR, CV, RPL) of the token-by-token kernels: as few lanes per row as its columns need, and no more rows per lane than there are.
 template <class F>
-hipError_t by_columns(int cols, F go) {      // LPR, CV
-    if (cols <= 16) return go(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
-    if (cols <= 32) return go(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
-    if (cols <= 64) return go(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    return go(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+hipError_t by_shape(int rows, int cols, F go) {
+    auto with = [&](auto lpr, auto cv) {
+        constexpr int RW = 64 / lpr.value;
+        if (rows <= RW) return go(lpr, cv, std::integral_constant<int, 1>());
+        if (rows <= 2 * RW) return go(lpr, cv, std::integral_constant<int, 2>());
+        return go(lpr, cv, std::integral_constant<int, 4>());
+    };
+    if (cols <= 16) return with(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    if (cols <= 32) return with(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+    if (cols <= 64) return with(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    return with(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
 }
+
+// States of a call from which on they pass the caches by.
+constexpr size_t STREAM_BYTES = (size_t)64 << 20;
 
 // Token by token: the passes of the job, all with rows and columns of the same sizes.
 template <class T>
 hipError_t launch_recurrent(const DecayJob &job, int passes, int heads, hipStream_t s) {
-    return by_columns(job.pass[0].cols, [&](auto lpr, auto cv) {
-        constexpr int ROWS = 4 * (64 / lpr.value) * DR_RPL;
-        const int slices = (job.pass[0].rows + ROWS - 1) / ROWS;
-        launch(decay_recurrent_kernel<T, lpr.value, cv.value>, dim3(job.n_segments, heads, passes * slices), dim3(256), 0, s, job, slices);
+    return by_shape(job.pass[0].rows, job.pass[0].cols, [&](auto lpr, auto cv, auto rpl) {
+        constexpr int ROWS = 64 / lpr.value * rpl.value;
+        const int slabs = (job.pass[0].rows + ROWS - 1) / ROWS;
+        const int64_t units = (int64_t)job.n_segments * slabs;
+        launch(decay_recurrent_kernel<T, lpr.value, cv.value, rpl.value>, dim3((unsigned)((units + 3) / 4), heads, passes), dim3(256), 0, s, job, slabs);
         return hipGetLastError();
     });
 }
@@ -777,13 +881,14 @@ int span_of(int heads, int n_segments, int n_tokens) {
 constexpr int BRIEF = 32;
 
 void plan(DecayJob &job, int heads) {
-    job.span = span_of(heads, job.n_segments, job.n_tokens);
-    job.items = job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
     job.brief = job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
+    job.span = job.brief >= 0 ? 1 << 30 : span_of(heads, job.n_segments, job.n_tokens);
+    job.items = job.brief >= 0 ? job.n_tokens / (job.brief + 1) + 1
+                               : job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
 }
 size_t spans_floats(const DecayJob &job, int heads, size_t size) {
     const int longest = job.seg_start ? job.n_tokens : job.len;
-    return longest <= job.span || longest <= job.brief ? 0 : (size_t)job.items * heads * (size + 1);
+    return longest <= job.span ? 0 : (size_t)job.items * heads * (size + 1);
 }
 
 // passes: of outputs; sources: those of them whose spans' states are made (one forward, one backward)
@@ -793,7 +898,7 @@ hipError_t run_job(DecayJob &job, int passes, const int *sources, int n_sources,
     hipError_t e = hipSuccess;
     if (job.brief >= 0 && (job.seg_start || longest <= job.brief))
         e = by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_recurrent<T>(some, n, heads, s); });
-    if (e != hipSuccess || (job.brief >= 0 && longest <= job.brief)) return e;
+    if (e != hipSuccess || longest <= job.brief) return e;
     if (longest > job.span) {
         DecayJob made = job;
         for (int i = 0; i < n_sources; ++i) made.pass[i] = job.pass[sources[i]];
@@ -845,7 +950,7 @@ int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *
 }
 int check_segments(const int32_t *seg_start, int n_segments, int n_tokens, const char *who) {
     if (n_segments < 0 || n_tokens < 0) return call_fail(GA3C_EINVAL, "%s: negative count", who);
-    if (n_segments > 1 << 30) return call_fail(GA3C_EINVAL, "%s: more than 2^30 segments", who);
+    if (n_segments > 1 << 24) return call_fail(GA3C_EINVAL, "%s: more than 2^24 segments", who);
     if (n_segments == 0 && n_tokens > 0) return call_fail(GA3C_EINVAL, "%s: tokens without a segment", who);
     if (!seg_start && n_segments > 0 && n_tokens % n_segments) return call_fail(GA3C_EINVAL, "%s: %d tokens are no %d equal segments", who, n_tokens, n_segments);
     return GA3C_OK;
@@ -959,14 +1064,18 @@ extern "C" int ga3c_decay_attention_step(const ga3c_decay_desc *d, const ga3c_he
     p.key = d->key_dim; p.value = d->value_dim; p.slots = slots; p.starts = starts; p.states = states; p.n = n; p.n_slots = n_slots;
     p.scale = d->scale;
     memcpy(p.decay, d->decay, sizeof(float) * d->n_heads);
-    const hipError_t e = by_columns(p.key, [&](auto lpr, auto cv) {
-        constexpr int ROWS = 4 * (64 / lpr.value) * DR_RPL;
-        const dim3 grid(n, d->n_heads, (p.value + ROWS - 1) / ROWS);
-        const bool states4 = (uintptr_t)states % 16 == 0;
-        if (d->dtype == GA3C_BF16)
-            launch(decay_step_kernel<bf16, lpr.value, cv.value>, grid, dim3(256), 0, (hipStream_t)stream, p, (int)(states4 && rows_of_four<bf16>(p.k) && rows_of_four<bf16>(p.q)));
-        else
-            launch(decay_step_kernel<float, lpr.value, cv.value>, grid, dim3(256), 0, (hipStream_t)stream, p, (int)(states4 && rows_of_four<float>(p.k) && rows_of_four<float>(p.q)));
+    const hipStream_t s = (hipStream_t)stream;
+    const hipError_t e = by_shape(p.value, p.key, [&](auto lpr, auto cv, auto rpl) {
+        constexpr int ROWS = 64 / lpr.value * rpl.value;
+        const int slabs = (p.value + ROWS - 1) / ROWS;
+        const dim3 grid((unsigned)(((int64_t)n * slabs + 3) / 4), d->n_heads);
+        const bool bf = d->dtype == GA3C_BF16;
+        const int vec = bf ? rows_of_four<bf16>(p.k) && rows_of_four<bf16>(p.q) : rows_of_four<float>(p.k) && rows_of_four<float>(p.q);
+        const bool stream_states = p.key % 4 == 0 && (uintptr_t)states % 16 == 0 && (size_t)n * d->n_heads * p.key * p.value * sizeof(float) >= STREAM_BYTES;
+        typedef void (*Kernel)(DecayStep, int, int);
+        static const Kernel kernels[4] = {decay_step_kernel<float, lpr.value, cv.value, rpl.value, false>, decay_step_kernel<float, lpr.value, cv.value, rpl.value, true>,
+                                          decay_step_kernel<bf16, lpr.value, cv.value, rpl.value, false>, decay_step_kernel<bf16, lpr.value, cv.value, rpl.value, true>};
+        launch(kernels[2 * bf + stream_states], grid, dim3(256), 0, s, p, slabs, vec);
         return hipGetLastError();
     });
     return hip_result(e, who);
