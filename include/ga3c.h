@@ -507,7 +507,9 @@ int ga3c_decay_attention_step(const ga3c_decay_desc *desc, const ga3c_heads *q, 
  *   y = act((x - mean) * rstd * gamma + beta),  rstd = 1 / sqrt(var + eps)
  * with mean and (biased) variance over the sample's group, gamma and beta f32
  * [channels].  Position i of x starts at x + i * x_stride elements, i counting
- * through all samples; x_stride, y_stride >= channels.
+ * through all samples; x_stride, y_stride >= channels.  At most 2^20 channels,
+ * 2^24 samples and 2^24 positions; a sample far larger than a few GB may be
+ * refused.
  *   stats_dev   f32 [n_samples][groups][2] receives mean and rstd, which the
  *               gradient needs; may be NULL
  *   workspace_dev  as above, of ga3c_group_norm_workspace() bytes
