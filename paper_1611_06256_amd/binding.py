@@ -8,7 +8,9 @@ the calls raise.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence, Tuple
 
@@ -190,7 +192,7 @@ def load_library() -> C.CDLL:
     lib.ga3c_tuner_set_margin.argtypes = [vp, C.c_double]
     lib.ga3c_tuner_progress.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
     lib.ga3c_use_generic_kernels.argtypes = [vp, i32]
-    heads, i64 = C.POINTER(_Heads), C.c_int64
+    heads, i64 = vp, C.c_int64          # heads: addresses of _Heads
     lib.ga3c_decay_attention.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, i32, vp, vp, vp, sz, vp]
     lib.ga3c_decay_attention_grad.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 7 + [vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.ga3c_decay_attention_step.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, vp, i32, vp]
@@ -547,52 +549,71 @@ def rmsprop_flat(theta, g, grad, scale: float, lr: float, rms_decay: float, rms_
 
 
 # ------------------------------------------------------------- memory of an agent --
+#
+# These calls take a few microseconds on the GPU, so what they cost on the host counts: tensors are checked with few
+# attribute reads, and the views that the C ABI takes by address are packed into one buffer.
 
-def _on_device(t, what: str) -> None:
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise Ga3cError(f"{what}: expected a GPU tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise Ga3cError(f"{what}: on {t.device}, which is not the current device")
+_HEADS_SIZE = C.sizeof(_Heads)
+_element_types = {}
 
 
 def _element_type(t, what: str) -> int:
+    """GA3C_F32 or GA3C_BF16 of a tensor on the current device."""
     import torch
-    _on_device(t, what)
-    if t.dtype not in (torch.float32, torch.bfloat16):
+    if not _element_types:
+        _element_types.update({torch.float32: 0, torch.bfloat16: 1})
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise Ga3cError(f"{what}: expected a GPU tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise Ga3cError(f"{what}: on {t.device}, which is not the current device")
+    dtype = _element_types.get(t.dtype)
+    if dtype is None:
         raise Ga3cError(f"{what}: expected dtype torch.float32 or torch.bfloat16, got {t.dtype}")
-    return 0 if t.dtype == torch.float32 else 1
+    return dtype
 
 
-def _heads(t, like, dim: int, what: str):
-    """View of a tensor [tokens, heads, dim] of the type and leading sizes of `like`, elements of a row side by side."""
-    _on_device(t, what)
-    if t.dtype != like.dtype:
-        raise Ga3cError(f"{what}: expected dtype {like.dtype}, got {t.dtype}")
-    if tuple(t.shape) != (like.shape[0], like.shape[1], dim):
-        raise Ga3cError(f"{what}: expected shape {(like.shape[0], like.shape[1], dim)}, got {tuple(t.shape)}")
-    if t.stride(2) != 1 and dim > 1:
-        raise Ga3cError(f"{what}: the elements of a row must lie side by side")
-    return _Heads(t.data_ptr(), t.stride(0), t.stride(1))
+def _like(t, shape, dtype, device, what: str) -> None:
+    """t is a tensor of this shape and type on the device of the call."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise Ga3cError(f"{what}: expected a GPU tensor")
+    if t.device != device:
+        raise Ga3cError(f"{what}: on {t.device}, which is not the current device")
+    if t.dtype is not dtype:
+        raise Ga3cError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise Ga3cError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _flat(t, dtype, shape, what: str):
-    """Device pointer of a contiguous tensor of this shape; None stays None."""
+def _views(tensors, shapes, names, dtype, device):
+    """The ga3c_heads of tensors [tokens, heads, dim], one behind the other in a buffer: elements of a row side by side."""
+    out = []
+    for t, shape, what in zip(tensors, shapes, names):
+        _like(t, shape, dtype, device, what)
+        token, head, one = t.stride()
+        if one != 1 and shape[2] > 1:
+            raise Ga3cError(f"{what}: the elements of a row must lie side by side")
+        out += (t.data_ptr(), token, head)
+    return struct.pack(f"{len(out)}q", *out)
+
+
+def _flat(t, shape, dtype, device, what: str):
+    """Address of a contiguous tensor of this shape; None stays None."""
     if t is None:
         return None
-    _on_device(t, what)
-    if tuple(t.shape) != tuple(shape):
-        raise Ga3cError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _ptr(t, dtype, what)
+    _like(t, shape, dtype, device, what)
+    if not t.is_contiguous():
+        raise Ga3cError(f"{what}: tensor must be contiguous")
+    return t.data_ptr()
 
 
-def _given_stream(stream, t):
+def _raw_stream(stream, device) -> int:
     import torch
     if stream is None:
-        return torch.cuda.current_stream()
-    if stream.device != t.device:
-        raise Ga3cError(f"stream: on {stream.device}, the tensors on {t.device}")
-    return stream
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    if stream.device != device:
+        raise Ga3cError(f"stream: on {stream.device}, the tensors on {device}")
+    return stream.cuda_stream
 
 
 def _workspace(nbytes: int, stream):
@@ -600,25 +621,31 @@ def _workspace(nbytes: int, stream):
     import torch
     if nbytes == 0:
         return None
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
     with torch.cuda.stream(stream):
         return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
 
 
+@functools.lru_cache(maxsize=64)
+def _decay_desc_of(heads: int, key: int, value: int, dtype: int, decay: Tuple[float, ...], scale: float) -> _DecayDesc:
+    host = (C.c_float * max(1, heads))(*decay)
+    return _DecayDesc(heads, key, value, dtype, C.cast(host, C.POINTER(C.c_float)), scale)
+
+
 def _decay_desc(q, v, decay, scale: float) -> _DecayDesc:
+    dtype = _element_type(q, "q")
     for t, what in ((q, "q"), (v, "v")):
-        dtype = _element_type(t, what)
         if t.dim() != 3:
             raise Ga3cError(f"{what}: expected [tokens, heads, dim], got {tuple(t.shape)}")
     if len(decay) != q.shape[1]:
         raise Ga3cError(f"decay: expected one for each of {q.shape[1]} heads, got {len(decay)}")
-    host = (C.c_float * len(decay))(*[float(d) for d in decay])
-    return _DecayDesc(q.shape[1], q.shape[2], v.shape[2], dtype, C.cast(host, C.POINTER(C.c_float)), scale)
+    return _decay_desc_of(q.shape[1], q.shape[2], v.shape[2], dtype, tuple(decay), scale)
 
 
-def _segments(q, seg_start, segments, starts):
-    """Number of segments, and the device pointers of their table and of the starts."""
+def _segments(n: int, seg_start, segments, starts, device):
+    """Number of segments, and the addresses of their table and of the starts."""
     import torch
-    n = int(q.shape[0])
     if seg_start is not None:
         if seg_start.dim() != 1 or seg_start.numel() < 1:
             raise Ga3cError("seg_start: expected [segments + 1]")
@@ -627,7 +654,7 @@ def _segments(q, seg_start, segments, starts):
         segments = seg_start.numel() - 1
     elif segments is None:
         segments = 1 if n else 0
-    return segments, _flat(seg_start, torch.int32, (segments + 1,), "seg_start"), _flat(starts, torch.uint8, (n,), "starts")
+    return segments, _flat(seg_start, (segments + 1,), torch.int32, device, "seg_start"), _flat(starts, (n,), torch.uint8, device, "starts")
 
 
 def decay_attention(q, k, v, decay, out, seg_start=None, segments: Optional[int] = None, starts=None, state_in=None,
@@ -639,18 +666,21 @@ def decay_attention(q, k, v, decay, out, seg_start=None, segments: Optional[int]
     segments of equal length (one unless given).  starts u8 [tokens] or None; state_in, state_out f32 [segments, heads,
     value_dim, key_dim] or None.  out and state_out are filled."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     d = _decay_desc(q, v, decay, scale)
-    n, h, dk, dv = q.shape[0], d.n_heads, d.key_dim, d.value_dim
-    segments, table, begun = _segments(q, seg_start, segments, starts)
+    dev, by_key = q.device, q.shape
+    n, h, dk, dv = by_key[0], by_key[1], by_key[2], v.shape[2]
+    by_value = (n, h, dv)
+    segments, table, begun = _segments(n, seg_start, segments, starts, dev)
+    views = _views((q, k, v, out), (by_key, by_key, by_value, by_value), ("q", "k", "v", "out"), q.dtype, dev)
     state = (segments, h, dv, dk)
-    s = _given_stream(stream, q)
-    views = [_heads(q, q, dk, "q"), _heads(k, q, dk, "k"), _heads(v, q, dv, "v"), _heads(out, q, dv, "out")]
-    given = [_flat(state_in, torch.float32, state, "state_in"), _flat(state_out, torch.float32, state, "state_out")]
-    nbytes = lib.ga3c_decay_attention_workspace(C.byref(d), segments, n)
-    ws = _workspace(nbytes, s)
-    _check(lib.ga3c_decay_attention(C.byref(d), *[C.byref(x) for x in views], table, begun, segments, n, *given,
-                                    None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_decay_attention")
+    x_in, x_out = _flat(state_in, state, torch.float32, dev, "state_in"), _flat(state_out, state, torch.float32, dev, "state_out")
+    p = C.byref(d)
+    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n)
+    ws = _workspace(nbytes, stream)
+    at = C.cast(views, C.c_void_p).value
+    _check(lib.ga3c_decay_attention(p, at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE, table, begun, segments, n, x_in,
+                                    x_out, None if ws is None else ws.data_ptr(), nbytes, _raw_stream(stream, dev)), "ga3c_decay_attention")
 
 
 def decay_attention_grad(q, k, v, decay, dout, dq, dk, dv, seg_start=None, segments: Optional[int] = None, starts=None,
@@ -658,72 +688,85 @@ def decay_attention_grad(q, k, v, decay, dout, dq, dk, dv, seg_start=None, segme
     """Gradient of decay_attention: fills dq, dk, dv (shaped like q, k, v) and, if given, dstate_in, from dout and, if given,
     dstate_out.  The other arguments are those of the forward call."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     d = _decay_desc(q, v, decay, scale)
-    n, h, kd, vd = q.shape[0], d.n_heads, d.key_dim, d.value_dim
-    segments, table, begun = _segments(q, seg_start, segments, starts)
+    dev, by_key = q.device, q.shape
+    n, h, kd, vd = by_key[0], by_key[1], by_key[2], v.shape[2]
+    by_value = (n, h, vd)
+    segments, table, begun = _segments(n, seg_start, segments, starts, dev)
+    views = _views((q, k, v, dout, dq, dk, dv), (by_key, by_key, by_value, by_value, by_key, by_key, by_value),
+                   ("q", "k", "v", "dout", "dq", "dk", "dv"), q.dtype, dev)
     state = (segments, h, vd, kd)
-    s = _given_stream(stream, q)
-    views = [_heads(q, q, kd, "q"), _heads(k, q, kd, "k"), _heads(v, q, vd, "v"), _heads(dout, q, vd, "dout"),
-             _heads(dq, q, kd, "dq"), _heads(dk, q, kd, "dk"), _heads(dv, q, vd, "dv")]
-    given = [_flat(state_in, torch.float32, state, "state_in"), _flat(dstate_out, torch.float32, state, "dstate_out"),
-             _flat(dstate_in, torch.float32, state, "dstate_in")]
-    nbytes = lib.ga3c_decay_attention_workspace(C.byref(d), segments, n)
-    ws = _workspace(nbytes, s)
-    _check(lib.ga3c_decay_attention_grad(C.byref(d), *[C.byref(x) for x in views], table, begun, segments, n, *given,
-                                         None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_decay_attention_grad")
+    x = [_flat(t, state, torch.float32, dev, what) for t, what in ((state_in, "state_in"), (dstate_out, "dstate_out"), (dstate_in, "dstate_in"))]
+    p = C.byref(d)
+    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n)
+    ws = _workspace(nbytes, stream)
+    at = C.cast(views, C.c_void_p).value
+    _check(lib.ga3c_decay_attention_grad(p, *range(at, at + 7 * _HEADS_SIZE, _HEADS_SIZE), table, begun, segments, n, *x,
+                                         None if ws is None else ws.data_ptr(), nbytes, _raw_stream(stream, dev)), "ga3c_decay_attention_grad")
 
 
 def decay_attention_step(q, k, v, decay, states, out, slots=None, starts=None, scale: float = 1.0, stream=None) -> None:
     """One token of each agent (ga3c_decay_attention_step): q, k [n, heads, key_dim]; v, out [n, heads, value_dim]; states f32
     [slots, heads, value_dim, key_dim], advanced in place; slots i32 [n] or None (token i has state i); starts u8 [n] or None."""
     import torch
+    lib = _lib or load_library()
     d = _decay_desc(q, v, decay, scale)
-    n, h, dk, dv = q.shape[0], d.n_heads, d.key_dim, d.value_dim
-    s = _given_stream(stream, q)
-    views = [_heads(q, q, dk, "q"), _heads(k, q, dk, "k"), _heads(v, q, dv, "v"), _heads(out, q, dv, "out")]
+    dev, by_key = q.device, q.shape
+    n, h, dk, dv = by_key[0], by_key[1], by_key[2], v.shape[2]
+    by_value = (n, h, dv)
+    views = _views((q, k, v, out), (by_key, by_key, by_value, by_value), ("q", "k", "v", "out"), q.dtype, dev)
     if not isinstance(states, torch.Tensor) or states.dim() != 4:
         raise Ga3cError("states: expected a GPU tensor [slots, heads, value_dim, key_dim]")
-    n_slots = int(states.shape[0])
-    _check(load_library().ga3c_decay_attention_step(C.byref(d), *[C.byref(x) for x in views], _flat(slots, torch.int32, (n,), "slots"),
-                                                    _flat(starts, torch.uint8, (n,), "starts"), n,
-                                                    _flat(states, torch.float32, (n_slots, h, dv, dk), "states"), n_slots,
-                                                    s.cuda_stream), "ga3c_decay_attention_step")
+    n_slots = states.shape[0]
+    at = C.cast(views, C.c_void_p).value
+    _check(lib.ga3c_decay_attention_step(C.byref(d), at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE,
+                                         _flat(slots, (n,), torch.int32, dev, "slots"), _flat(starts, (n,), torch.uint8, dev, "starts"), n,
+                                         _flat(states, (n_slots, h, dv, dk), torch.float32, dev, "states"), n_slots,
+                                         _raw_stream(stream, dev)), "ga3c_decay_attention_step")
 
 
 _ACT = {"none": 0, "relu": 1, "silu": 2}
 
 
 def _rows(t, like, what: str):
-    """Device pointer and position stride of [samples, ..., channels], positions evenly spaced through all samples."""
-    _on_device(t, what)
-    if t.dtype != like.dtype or t.shape != like.shape:
-        raise Ga3cError(f"{what}: expected {like.dtype} {tuple(like.shape)}, got {t.dtype} {tuple(t.shape)}")
-    if t.numel() == 0:
-        return C.c_void_p(t.data_ptr()), max(1, t.shape[-1])
+    """Address and position stride of [samples, ..., channels], positions evenly spaced through all samples."""
+    if t is not like:
+        _like(t, like.shape, like.dtype, like.device, what)
+    shape, step = t.shape, t.stride()
+    channels = shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), max(1, channels)
     stride, count = None, 1
-    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if size > 1:
+    for i in range(len(shape) - 2, -1, -1):
+        if shape[i] > 1:
             if stride is None:
-                stride = step
-            if step != stride * count:
+                stride = step[i]
+            if step[i] != stride * count:
                 raise Ga3cError(f"{what}: positions must be evenly spaced")
-        count *= size
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        count *= shape[i]
+    if channels > 1 and step[-1] != 1:
         raise Ga3cError(f"{what}: the channels of a position must lie side by side")
-    return C.c_void_p(t.data_ptr()), stride if stride is not None else t.shape[-1]
+    return t.data_ptr(), channels if stride is None else stride
+
+
+@functools.lru_cache(maxsize=64)
+def _norm_desc_of(channels: int, groups: int, dtype: int, act: int, eps: float) -> _NormDesc:
+    return _NormDesc(channels, groups, dtype, act, eps)
 
 
 def _norm_desc(x, groups: int, act: str, eps: float):
+    """Description, samples and positions."""
     dtype = _element_type(x, "x")
-    if x.dim() < 2:
-        raise Ga3cError(f"x: expected [samples, ..., channels], got {tuple(x.shape)}")
+    shape = x.shape
+    if len(shape) < 2:
+        raise Ga3cError(f"x: expected [samples, ..., channels], got {tuple(shape)}")
     if act not in _ACT:
         raise Ga3cError(f"act: expected one of {sorted(_ACT)}, got {act!r}")
     positions = 1
-    for size in x.shape[1:-1]:
-        positions *= int(size)
-    return _NormDesc(x.shape[-1], groups, dtype, _ACT[act], eps), int(x.shape[0]), positions
+    for size in shape[1:-1]:
+        positions *= size
+    return _norm_desc_of(shape[-1], groups, dtype, _ACT[act], eps), shape[0], positions
 
 
 def group_norm(x, gamma, beta, groups: int, y, stats=None, act: str = "none", eps: float = 1e-5, stream=None) -> None:
@@ -732,36 +775,35 @@ def group_norm(x, gamma, beta, groups: int, y, stats=None, act: str = "none", ep
     x, y [samples, ..., channels], float32 or bfloat16, positions evenly spaced; gamma, beta f32 [channels]; stats f32
     [samples, groups, 2] or None.  y and stats (mean and 1 / standard deviation) are filled."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     d, samples, positions = _norm_desc(x, groups, act, eps)
-    s = _given_stream(stream, x)
+    dev, f, each = x.device, torch.float32, (x.shape[-1],)
     xp, xs = _rows(x, x, "x")
     yp, ys = _rows(y, x, "y")
-    weights = [_flat(t, torch.float32, (d.channels,), what) for t, what in ((gamma, "gamma"), (beta, "beta"))]
-    st = _flat(stats, torch.float32, (samples, groups, 2), "stats")
-    nbytes = lib.ga3c_group_norm_workspace(C.byref(d), samples, positions)
-    ws = _workspace(nbytes, s)
-    _check(lib.ga3c_group_norm(C.byref(d), xp, xs, *weights, yp, ys, st, samples, positions,
-                               None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_group_norm")
+    p = C.byref(d)
+    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions)
+    ws = _workspace(nbytes, stream)
+    _check(lib.ga3c_group_norm(p, xp, xs, _flat(gamma, each, f, dev, "gamma"), _flat(beta, each, f, dev, "beta"), yp, ys,
+                               _flat(stats, (samples, groups, 2), f, dev, "stats"), samples, positions,
+                               None if ws is None else ws.data_ptr(), nbytes, _raw_stream(stream, dev)), "ga3c_group_norm")
 
 
 def group_norm_grad(x, dy, gamma, beta, stats, groups: int, dx, dgamma, dbeta, act: str = "none", stream=None) -> None:
     """Gradient of group_norm: fills dx (shaped like x), dgamma and dbeta f32 [channels] from dy and the forward call's stats."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     d, samples, positions = _norm_desc(x, groups, act, 0.0)
-    s = _given_stream(stream, x)
+    dev, f, each = x.device, torch.float32, (x.shape[-1],)
     xp, xs = _rows(x, x, "x")
     yp, ys = _rows(dy, x, "dy")
     dp, ds = _rows(dx, x, "dx")
-    f = torch.float32
-    weights = [_flat(gamma, f, (d.channels,), "gamma"), _flat(beta, f, (d.channels,), "beta"),
-               _flat(stats, f, (samples, groups, 2), "stats")]
-    dw = [_flat(dgamma, f, (d.channels,), "dgamma"), _flat(dbeta, f, (d.channels,), "dbeta")]
-    nbytes = lib.ga3c_group_norm_workspace(C.byref(d), samples, positions)
-    ws = _workspace(nbytes, s)
-    _check(lib.ga3c_group_norm_grad(C.byref(d), xp, xs, yp, ys, *weights, dp, ds, *dw, samples, positions,
-                                    None if ws is None else ws.data_ptr(), nbytes, s.cuda_stream), "ga3c_group_norm_grad")
+    p = C.byref(d)
+    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions)
+    ws = _workspace(nbytes, stream)
+    _check(lib.ga3c_group_norm_grad(p, xp, xs, yp, ys, _flat(gamma, each, f, dev, "gamma"), _flat(beta, each, f, dev, "beta"),
+                                    _flat(stats, (samples, groups, 2), f, dev, "stats"), dp, ds, _flat(dgamma, each, f, dev, "dgamma"),
+                                    _flat(dbeta, each, f, dev, "dbeta"), samples, positions,
+                                    None if ws is None else ws.data_ptr(), nbytes, _raw_stream(stream, dev)), "ga3c_group_norm_grad")
 
 
 def stats_from_tensor(t) -> Dict[str, float]:
