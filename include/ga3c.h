@@ -486,8 +486,8 @@ int ga3c_decay_attention_grad(const ga3c_decay_desc *desc, const ga3c_heads *q, 
                               const float *state_in_dev, const float *dstate_out_dev, float *dstate_in_dev,
                               void *workspace_dev, size_t workspace_bytes, void *stream);
 
-/* Scratch for either call, in bytes (0 for a bad description). */
-size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *desc, int n_segments, int n_tokens);
+/* Scratch for the gradient (grad != 0) or the forward call, in bytes (0 for a bad description). */
+size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *desc, int n_segments, int n_tokens, int grad);
 
 /* One token of each of n agents, whose states lie in states_dev f32
  * [n_slots][n_heads][value_dim][key_dim] and are advanced in place.
@@ -531,7 +531,47 @@ int ga3c_group_norm_grad(const ga3c_norm_desc *desc, const void *x_dev, int64_t 
                          int64_t dy_stride, const float *gamma_dev, const float *beta_dev, const float *stats_dev,
                          void *dx_dev, int64_t dx_stride, float *dgamma_dev, float *dbeta_dev, int n_samples,
                          int n_positions, void *workspace_dev, size_t workspace_bytes, void *stream);
-size_t ga3c_group_norm_workspace(const ga3c_norm_desc *desc, int n_samples, int n_positions);
+size_t ga3c_group_norm_workspace(const ga3c_norm_desc *desc, int n_samples, int n_positions, int grad);
+
+/* A network with a memory between the fc layer and the heads.  The fc layer's
+ * units, behind their rectifier, are x = [queries | keys | values] of the
+ * memory's heads: fc_units = heads * (2 key_dim + value_dim), each part head by
+ * head.  Per agent:
+ *   o  = attention with a decay for each head on them, scale 1 / sqrt(key_dim)
+ *   n  = max(0, group norm of o, a group per head, eps 1e-5, with weights gamma, beta)
+ * and the heads take x with n added to its values.  The flat parameter vector
+ * has gamma [heads * value_dim] and beta [heads * value_dim] between fc b and
+ * policy W; ga3c_params_offsets gives their offsets behind the total, two
+ * entries more.  ga3c_params_init sets gamma to 1, beta to 0.  math must be 0.
+ * Everything else a context can do it does as before, but for ga3c_predict,
+ * ga3c_train_step, ga3c_train_step_ragged and ga3c_sched_create, which refuse it. */
+#define GA3C_MAX_MEMORY_HEADS 16
+typedef struct {
+    int heads, key_dim, value_dim;
+    float decay[GA3C_MAX_MEMORY_HEADS];     /* of the first `heads`, each in [0, 1] */
+} ga3c_memory_desc;
+int ga3c_create_memory(const ga3c_net_desc *desc, const ga3c_memory_desc *memory, int max_predict_batch,
+                       int max_train_frames, ga3c_ctx **out);
+
+/* ga3c_predict, one step of each agent.  agents_dev i32 [B], starts_dev u8 [B]
+ * and states_dev f32 [n_agents][heads][value_dim][key_dim] are the slots,
+ * starts and states of ga3c_decay_attention_step: an agent's state is advanced
+ * in place by its frame, and is zero where its episode begins.  (Keep a copy of
+ * the states that a segment begins with for the update on it.) */
+int ga3c_predict_memory(ga3c_ctx *ctx, const uint8_t *frames_dev, int B, const int32_t *agents_dev,
+                        const uint8_t *starts_dev, float *states_dev, int n_agents, const float *uniforms_dev,
+                        float *logits_dev, float *values_dev, float *probs_dev, int32_t *actions_dev, void *stream);
+
+/* One update, on N segments of equal length (seg_start_dev NULL, n_frames a
+ * multiple of N; as ga3c_train_step) or not (as ga3c_train_step_ragged).
+ * states_dev f32 [N][heads][value_dim][key_dim]: the state of each segment's
+ * agent before its first frame (zeros where an episode begins there), or NULL =
+ * zero; no gradient goes into them.  Inside a segment the memory is cleared
+ * behind a frame whose dones is non-zero. */
+int ga3c_train_step_memory(ga3c_ctx *ctx, const uint8_t *frames_dev, const int32_t *actions_dev,
+                           const float *rewards_dev, const uint8_t *dones_dev, const int32_t *seg_start_dev,
+                           const float *states_dev, const float *bootstrap_dev, int N, int n_frames,
+                           const ga3c_hparams *hp, ga3c_train_stats *stats_dev, void *stream);
 
 /* Thread-local text of the last error on this thread ("" if none). */
 const char *ga3c_last_error(void);

@@ -58,6 +58,10 @@ class _NormDesc(C.Structure):
     _fields_ = [("channels", C.c_int), ("groups", C.c_int), ("dtype", C.c_int), ("act", C.c_int), ("eps", C.c_float)]
 
 
+class _MemoryDesc(C.Structure):
+    _fields_ = [("heads", C.c_int), ("key_dim", C.c_int), ("value_dim", C.c_int), ("decay", C.c_float * 16)]
+
+
 class Prediction(C.Structure):
     _fields_ = [("agent", C.c_int32), ("action", C.c_int32), ("value", C.c_float), ("policy_version", C.c_int32)]
 
@@ -97,6 +101,20 @@ class NetDesc:
             d.conv[i].oc, d.conv[i].k, d.conv[i].stride = oc, k, s
         d.fc_units, d.n_actions, d.math = self.fc_units, self.n_actions, self.math
         return d
+
+
+@dataclass
+class MemoryDesc:
+    """Memory between the fc layer and the heads: heads * (2 * key_dim + value_dim) are the fc layer's units; a decay per head."""
+    heads: int = 4
+    key_dim: int = 16
+    value_dim: int = 32
+    decay: Sequence[float] = (0.75, 0.9375, 0.984375, 0.99609375)
+
+    def c(self) -> _MemoryDesc:
+        if len(self.decay) != self.heads or self.heads > 16:
+            raise Ga3cError(f"decay: expected one for each of {self.heads} heads (16 at most), got {len(self.decay)}")
+        return _MemoryDesc(self.heads, self.key_dim, self.value_dim, (C.c_float * 16)(*self.decay))
 
 
 def SMALL_NET(n_actions: int = 18) -> NetDesc:
@@ -140,6 +158,7 @@ EXPORTS = ("ga3c_create", "ga3c_destroy", "ga3c_params_count", "ga3c_params_offs
            "ga3c_sched_tick", "ga3c_sched_poll", "ga3c_sched_drain", "ga3c_sched_get_stats", "ga3c_sched_last_error",
            "ga3c_tuner_create", "ga3c_tuner_report", "ga3c_tuner_state", "ga3c_tuner_destroy", "ga3c_tuner_set_margin",
            "ga3c_tuner_progress",
+           "ga3c_create_memory", "ga3c_predict_memory", "ga3c_train_step_memory",
            "ga3c_decay_attention", "ga3c_decay_attention_grad", "ga3c_decay_attention_step", "ga3c_decay_attention_workspace",
            "ga3c_group_norm", "ga3c_group_norm_grad", "ga3c_group_norm_workspace")
 
@@ -192,15 +211,18 @@ def load_library() -> C.CDLL:
     lib.ga3c_tuner_set_margin.argtypes = [vp, C.c_double]
     lib.ga3c_tuner_progress.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
     lib.ga3c_use_generic_kernels.argtypes = [vp, i32]
+    lib.ga3c_create_memory.argtypes = [C.POINTER(_NetDesc), C.POINTER(_MemoryDesc), i32, i32, C.POINTER(vp)]
+    lib.ga3c_predict_memory.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.ga3c_train_step_memory.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, C.POINTER(_HParams), vp, vp]
     heads, i64 = vp, C.c_int64          # heads: addresses of _Heads
     lib.ga3c_decay_attention.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, i32, vp, vp, vp, sz, vp]
     lib.ga3c_decay_attention_grad.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 7 + [vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.ga3c_decay_attention_step.argtypes = [C.POINTER(_DecayDesc)] + [heads] * 4 + [vp, vp, i32, vp, i32, vp]
-    lib.ga3c_decay_attention_workspace.argtypes = [C.POINTER(_DecayDesc), i32, i32]
+    lib.ga3c_decay_attention_workspace.argtypes = [C.POINTER(_DecayDesc), i32, i32, i32]
     lib.ga3c_decay_attention_workspace.restype = sz
     lib.ga3c_group_norm.argtypes = [C.POINTER(_NormDesc), vp, i64, vp, vp, vp, i64, vp, i32, i32, vp, sz, vp]
     lib.ga3c_group_norm_grad.argtypes = [C.POINTER(_NormDesc), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i32, i32, vp, sz, vp]
-    lib.ga3c_group_norm_workspace.argtypes = [C.POINTER(_NormDesc), i32, i32]
+    lib.ga3c_group_norm_workspace.argtypes = [C.POINTER(_NormDesc), i32, i32, i32]
     lib.ga3c_group_norm_workspace.restype = sz
     lib.ga3c_profile_read.argtypes = [vp, C.c_char_p, sz]
     _lib = lib
@@ -235,16 +257,22 @@ def _stream(stream) -> C.c_void_p:
 class Ga3c:
     """One network on the current GPU: ga3c_create .. ga3c_destroy."""
 
-    def __init__(self, desc: NetDesc, max_predict_batch: int, max_train_frames: int):
+    def __init__(self, desc: NetDesc, max_predict_batch: int, max_train_frames: int, memory: Optional[MemoryDesc] = None):
         import torch
         if not torch.cuda.is_available():
             raise Ga3cError("no GPU visible: the HIP path has no CPU fallback")
         self._lib = load_library()
         self.desc = desc
         self._ctx = C.c_void_p()
+        self.memory = memory
         cd = desc.c()
-        _check(self._lib.ga3c_create(C.byref(cd), max_predict_batch, max_train_frames, C.byref(self._ctx)),
-               "ga3c_create")
+        if memory is None:
+            _check(self._lib.ga3c_create(C.byref(cd), max_predict_batch, max_train_frames, C.byref(self._ctx)),
+                   "ga3c_create")
+        else:
+            md = memory.c()
+            _check(self._lib.ga3c_create_memory(C.byref(cd), C.byref(md), max_predict_batch, max_train_frames, C.byref(self._ctx)),
+                   "ga3c_create_memory")
         self.n_params = int(self._lib.ga3c_params_count(self._ctx))
         self.n_actions = desc.n_actions
 
@@ -261,7 +289,7 @@ class Ga3c:
 
     def offsets(self) -> Dict[str, Tuple[int, Tuple[int, ...]]]:
         """Name -> (offset, shape) of each tensor in the flat parameter vector."""
-        off = (C.c_int64 * (2 * MAX_CONV + 7))()
+        off = (C.c_int64 * (2 * MAX_CONV + 9))()
         n = self._lib.ga3c_params_offsets(self._ctx, off, len(off))
         _check(n, "ga3c_params_offsets")
         o = [int(off[i]) for i in range(n)]
@@ -279,6 +307,9 @@ class Ga3c:
         out["policy.b"] = (o[nb + 3], (d.n_actions,))
         out["value.W"] = (o[nb + 4], (1, d.fc_units))
         out["value.b"] = (o[nb + 5], (1,))
+        if self.memory is not None:
+            read_out = self.memory.heads * self.memory.value_dim
+            out["memory.gamma"], out["memory.beta"] = (o[nb + 7], (read_out,)), (o[nb + 8], (read_out,))
         return out
 
     def params_init(self, seed: int, stream=None) -> None:
@@ -343,6 +374,65 @@ class Ga3c:
             _ptr(rewards, torch.float32, "rewards"), _ptr(dones, torch.uint8, "dones"),
             _ptr(seg_start, torch.int32, "seg_start"), _ptr(bootstrap, torch.float32, "bootstrap"),
             N, F, C.byref(hpc), sp, _stream(stream)), "ga3c_train_step_ragged")
+
+    def memory_states(self, n: int):
+        """States of n agents whose episodes have not begun: f32 [n, heads, value_dim, key_dim] of zeros."""
+        import torch
+        m = self.memory
+        if m is None:
+            raise Ga3cError("memory_states: the network has no memory")
+        return torch.zeros(n, m.heads, m.value_dim, m.key_dim, device="cuda")
+
+    def _states(self, states, n: int, what: str):
+        import torch
+        m = self.memory
+        if m is None:
+            raise Ga3cError(f"{what}: the network has no memory")
+        if states is not None and tuple(states.shape) != (n, m.heads, m.value_dim, m.key_dim):
+            raise Ga3cError(f"{what}: expected states {(n, m.heads, m.value_dim, m.key_dim)}, got {tuple(states.shape)}")
+        return _ptr(states, torch.float32, "states")
+
+    def predict_memory(self, frames, states, agents=None, starts=None, uniforms=None, logits=None, values=None, probs=None, actions=None,
+                       stream=None):
+        """One step of each agent of a network with a memory: frames u8 [B,C,H,W]; states f32 [n, heads, value_dim, key_dim], advanced
+        in place; agents i32 [B], the state of each frame, or None (frame i has state i); starts u8 [B] or None, non-zero where an
+        episode begins.  Output tensors that are passed in are filled."""
+        import torch
+        B, n = int(frames.shape[0]), int(states.shape[0])
+        for t, what in ((agents, "agents"), (starts, "starts")):
+            if t is not None and t.numel() != B:
+                raise Ga3cError(f"{what}: expected {B} entries")
+        _check(self._lib.ga3c_predict_memory(self._ctx, _ptr(frames, torch.uint8, "frames"), B, _ptr(agents, torch.int32, "agents"),
+                                             _ptr(starts, torch.uint8, "starts"), self._states(states, n, "predict_memory"), n,
+                                             _ptr(uniforms, torch.float32, "uniforms"),
+                                             _ptr(logits, torch.float32, "logits"), _ptr(values, torch.float32, "values"),
+                                             _ptr(probs, torch.float32, "probs"), _ptr(actions, torch.int32, "actions"),
+                                             _stream(stream)), "ga3c_predict_memory")
+
+    def train_step_memory(self, frames, actions, rewards, dones, bootstrap, hp: HParams, seg_start=None, states=None, stats=None,
+                          stream=None) -> None:
+        """One update of a network with a memory.  Without seg_start: frames u8 [N,T,C,H,W] and the rest as for train_step; with it:
+        frames u8 [F,C,H,W] and the rest as for train_step_ragged.  states f32 [N, heads, value_dim, key_dim], the state of each
+        segment's agent before its first frame, or None (zero); they are not changed."""
+        import torch
+        if seg_start is None:
+            N, F = int(frames.shape[0]), int(frames.shape[0]) * int(frames.shape[1])
+        else:
+            N, F = int(seg_start.numel()) - 1, int(frames.shape[0])
+        if actions.numel() != F or rewards.numel() != F or dones.numel() != F or N < 0 or \
+                (bootstrap is not None and bootstrap.numel() != N):
+            raise Ga3cError("train_step_memory: array sizes do not match the frame or segment count")
+        hpc = hp.c()
+        sp = None
+        if stats is not None:
+            if not stats.is_cuda or stats.numel() * stats.element_size() < C.sizeof(TrainStats):
+                raise Ga3cError("stats: need a GPU tensor of at least 24 bytes")
+            sp = C.c_void_p(stats.data_ptr())
+        _check(self._lib.ga3c_train_step_memory(
+            self._ctx, _ptr(frames, torch.uint8, "frames"), _ptr(actions, torch.int32, "actions"),
+            _ptr(rewards, torch.float32, "rewards"), _ptr(dones, torch.uint8, "dones"), _ptr(seg_start, torch.int32, "seg_start"),
+            self._states(states, N, "train_step_memory"), _ptr(bootstrap, torch.float32, "bootstrap"),
+            N, F, C.byref(hpc), sp, _stream(stream)), "ga3c_train_step_memory")
 
     def use_generic_kernels(self, on: bool) -> None:
         _check(self._lib.ga3c_use_generic_kernels(self._ctx, 1 if on else 0), "ga3c_use_generic_kernels")
@@ -676,7 +766,7 @@ def decay_attention(q, k, v, decay, out, seg_start=None, segments: Optional[int]
     state = (segments, h, dv, dk)
     x_in, x_out = _flat(state_in, state, torch.float32, dev, "state_in"), _flat(state_out, state, torch.float32, dev, "state_out")
     p = C.byref(d)
-    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n)
+    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n, 0)
     ws = _workspace(nbytes, stream)
     at = C.cast(views, C.c_void_p).value
     _check(lib.ga3c_decay_attention(p, at, at + _HEADS_SIZE, at + 2 * _HEADS_SIZE, at + 3 * _HEADS_SIZE, table, begun, segments, n, x_in,
@@ -699,7 +789,7 @@ def decay_attention_grad(q, k, v, decay, dout, dq, dk, dv, seg_start=None, segme
     state = (segments, h, vd, kd)
     x = [_flat(t, state, torch.float32, dev, what) for t, what in ((state_in, "state_in"), (dstate_out, "dstate_out"), (dstate_in, "dstate_in"))]
     p = C.byref(d)
-    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n)
+    nbytes = lib.ga3c_decay_attention_workspace(p, segments, n, 1)
     ws = _workspace(nbytes, stream)
     at = C.cast(views, C.c_void_p).value
     _check(lib.ga3c_decay_attention_grad(p, *range(at, at + 7 * _HEADS_SIZE, _HEADS_SIZE), table, begun, segments, n, *x,
@@ -781,7 +871,7 @@ def group_norm(x, gamma, beta, groups: int, y, stats=None, act: str = "none", ep
     xp, xs = _rows(x, x, "x")
     yp, ys = _rows(y, x, "y")
     p = C.byref(d)
-    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions)
+    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions, 0)
     ws = _workspace(nbytes, stream)
     _check(lib.ga3c_group_norm(p, xp, xs, _flat(gamma, each, f, dev, "gamma"), _flat(beta, each, f, dev, "beta"), yp, ys,
                                _flat(stats, (samples, groups, 2), f, dev, "stats"), samples, positions,
@@ -798,7 +888,7 @@ def group_norm_grad(x, dy, gamma, beta, stats, groups: int, dx, dgamma, dbeta, a
     yp, ys = _rows(dy, x, "dy")
     dp, ds = _rows(dx, x, "dx")
     p = C.byref(d)
-    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions)
+    nbytes = lib.ga3c_group_norm_workspace(p, samples, positions, 1)
     ws = _workspace(nbytes, stream)
     _check(lib.ga3c_group_norm_grad(p, xp, xs, yp, ys, _flat(gamma, each, f, dev, "gamma"), _flat(beta, each, f, dev, "beta"),
                                     _flat(stats, (samples, groups, 2), f, dev, "stats"), dp, ds, _flat(dgamma, each, f, dev, "dgamma"),

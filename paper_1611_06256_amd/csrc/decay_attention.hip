@@ -873,16 +873,17 @@ hipError_t by_sizes(const DecayJob &job, int passes, F go) {
 
 // Tokens that a block of the chunked kernels takes.  Spans of a segment cost its keys and values read twice and two states each,
 // so there are no more of them than it takes to give every compute unit a block.
-int span_of(int heads, int n_segments, int n_tokens) {
+constexpr int SHORTEST_SPAN = 256;
+int span_of(int heads, int n_tokens) {
     const int64_t want = (int64_t)n_tokens * heads / 256;
-    return (int)std::min<int64_t>(1 << 20, std::max<int64_t>(256, (want + 63) / 64 * 64));
+    return (int)std::min<int64_t>(1 << 20, std::max<int64_t>(SHORTEST_SPAN, (want + 63) / 64 * 64));
 }
 // Segments of up to so many tokens take the token-by-token kernel if the average is short.
 constexpr int BRIEF = 32;
 
 void plan(DecayJob &job, int heads) {
     job.brief = job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
-    job.span = job.brief >= 0 ? 1 << 30 : span_of(heads, job.n_segments, job.n_tokens);
+    job.span = job.brief >= 0 ? 1 << 30 : span_of(heads, job.n_tokens);
     job.items = job.brief >= 0 ? job.n_tokens / (job.brief + 1) + 1
                                : job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
 }
@@ -983,11 +984,18 @@ int hip_result(hipError_t e, const char *who) { return e == hipSuccess ? GA3C_OK
 
 using namespace ga3c;
 
-extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n_segments, int n_tokens) {
+extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n_segments, int n_tokens, int grad) {
     if (check_desc(d, "ga3c_decay_attention_workspace") != GA3C_OK || n_segments < 1 || n_tokens < 1) return 0;
     // as with a table, which needs the most; the gradient has states of both directions
     const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens);
-    return 2 * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
+    return (grad ? 2 : 1) * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
+}
+
+size_t ga3c::decay_workspace_most(const ga3c_decay_desc *d, int n_tokens) {
+    if (n_tokens <= SHORTEST_SPAN) return 0;
+    // segments that are not brief, and places for spans in between
+    const size_t items = (size_t)n_tokens / (BRIEF / 2 + 1) + 1 + n_tokens / SHORTEST_SPAN;
+    return 2 * sizeof(float) * items * d->n_heads * ((size_t)d->key_dim * d->value_dim + 1);
 }
 
 extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
@@ -1005,7 +1013,7 @@ extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *
         if (rc != GA3C_OK) return rc;
     }
     if (overlap(state_in, state_out, state)) return call_fail(GA3C_EINVAL, "%s: state_out lies over state_in", who);
-    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens);
+    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens, 0);
     if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
     DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);
@@ -1030,7 +1038,7 @@ extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_he
         if (rc != GA3C_OK) return rc;
     }
     if (overlap(state_in, dstate_in, state) || overlap(dstate_out, dstate_in, state)) return call_fail(GA3C_EINVAL, "%s: dstate_in lies over an input", who);
-    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens);
+    const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens, 1);
     if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
     DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);

@@ -35,4 +35,7 @@ struct DecayJob {
     float decay[GA3C_MAX_HEADS];
 };
 
+// Scratch for a call on up to n_tokens tokens, in whatever segments, in bytes.
+size_t decay_workspace_most(const ga3c_decay_desc *d, int n_tokens);
+
 }  // namespace ga3c

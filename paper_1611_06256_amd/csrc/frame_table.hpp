@@ -9,6 +9,8 @@
 
 namespace ga3c {
 
+// Whether the context's network has a memory (the scheduler's queues know of none).
+bool has_memory(const ga3c_ctx *c);
 // Whether the context's first layer can (the shape-specific layer of the small and the larger net); other contexts take
 // contiguous frames only.
 bool takes_frame_table(const ga3c_ctx *c);

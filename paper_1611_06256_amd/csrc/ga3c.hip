@@ -18,6 +18,7 @@
 
 #include "../../include/ga3c.h"
 #include "call_error.hpp"
+#include "decay_attention.hpp"
 #include "frame_table.hpp"
 #include "problems.hpp"
 #include "conv_frame.hpp"
@@ -137,6 +138,11 @@ struct Work {            // activations of one call; predict and train own one e
     size_t ws_floats = 0;
     const float *fc_ws = nullptr;   // where the last forward left the fc partial sums, and how many
     int fc_nz = 1;
+    // with a memory: [2][cap][F], behind the middle the fc output behind its rectifier, in front of it, with zeros beside it, what the
+    // memory read out (the heads take the sum of both); and that before its norm [cap][heads * value_dim]
+    float *mem = nullptr, *mem_o = nullptr;
+    float *features(int F) const { return mem + (size_t)cap * F; }
+    float *read_out(int F, int B) const { return mem + (size_t)(cap - B) * F; }
     // which conv outputs are positive, where the next layer's input gradient wants bits, and whether this forward pass has left them
     PositiveBits bits[GA3C_MAX_CONV];
     bool bits_set[GA3C_MAX_CONV] = {false, false, false, false};
@@ -224,6 +230,13 @@ struct ga3c_ctx {
     float *scale;                 // clip scale of the last step (1 float)
     ga3c_train_stats *stats;      // stats of the last step
     int last_frames;
+    // memory between the fc layer and the heads (heads == 0: none)
+    ga3c_memory_desc memory;
+    int64_t off_gamma, off_beta;  // of its norm's weights in the flat vector
+    float *no_bias;               // [F] zeros: the fc bias is in front of the memory
+    float *mem_stats, *mem_do, *mem_dm;      // training: the norm's statistics, dL/d(mem_o), dL/d(fc output) by way of the memory
+    uint8_t *mem_starts;          // training: frames that an episode begins with, inside a segment
+    void *mem_ws; size_t mem_ws_bytes;
 };
 
 namespace {
@@ -2078,6 +2091,12 @@ int alloc_work(Work &w, const ga3c_ctx *c, int cap, bool training) {
         }
     HIP_TRY(hipMalloc(&w.h, sizeof(float) * (size_t)cap * c->F));
     HIP_TRY(hipMalloc(&w.zv, sizeof(float) * (size_t)cap * (c->A + 1)));
+    if (c->memory.heads) {
+        const size_t floats = 2 * (size_t)cap * c->F;
+        HIP_TRY(hipMalloc(&w.mem, sizeof(float) * floats));
+        HIP_TRY(hipMemset(w.mem, 0, sizeof(float) * floats));
+        HIP_TRY(hipMalloc(&w.mem_o, sizeof(float) * (size_t)cap * c->memory.heads * c->memory.value_dim));
+    }
     return GA3C_OK;
 }
 
@@ -2086,6 +2105,7 @@ void free_work(Work &w) {
     for (int l = 0; l < GA3C_MAX_CONV; ++l) { (void)hipFree(w.act[l]); (void)hipFree(w.bits[l].at); }
     (void)hipFree(w.h);
     (void)hipFree(w.zv);
+    (void)hipFree(w.mem); (void)hipFree(w.mem_o);
 }
 
 // Tile shapes: output channels are few (16..64), pixels are many.
@@ -2190,6 +2210,50 @@ int small_launch_frames(const ga3c_ctx *c) {
     const int nb = 2 * c->nconv;
     if (c->nconv != 2 || c->F != SP_FC || c->flat != SP_FLAT || c->off[nb + 1] % 4 != 0 || c->off[nb + 2] % 4 != 0) return 0;
     return SpLds<2>::bytes(c->A) <= HEADS_FWD_MAX_LDS ? SP_MAX_FRAMES : SP_ONE_FRAME;
+}
+
+// The heads on the fc layer's partial sums (nz of them) and its bias; outputs to the optional pointers.
+int run_heads(ga3c_ctx *c, int which, Work &w, const float *fc_ws, int fc_nz, const float *fc_bias, int B, bool keep_zv, float *logits, float *values,
+              float *probs, const float *uniforms, int32_t *actions, hipStream_t s) {
+    const float *th = c->theta2[which];
+    const int nb = 2 * c->nconv;
+    const int hf = heads_loads(c->F, fc_nz, fc_ws, fc_bias, w.h, th + c->off[nb + 2]);
+    const int nj = c->F % 256 == 0 ? c->F / 256 : 0;
+    if (c->fast && !keep_zv && hf != LOADS_SCALAR && (nj == 1 || nj == 2 || nj == 4)) {
+        typedef decltype(&heads_predict_kernel<1, 8>) HeadsPredict;
+        static const HeadsPredict hp_kernels[6] = {heads_predict_kernel<1, 8>, heads_predict_kernel<1, 20>, heads_predict_kernel<2, 8>,
+                                                   heads_predict_kernel<2, 16>, heads_predict_kernel<4, 8>, heads_predict_kernel<4, 8>};
+        static size_t hp_lds_set[6] = {0, 0, 0, 0, 0, 0};
+        const int k = (nj == 1 ? 0 : nj == 2 ? 2 : 4) + (hf == LOADS_VEC16 ? 1 : 0);
+        const size_t lds = sizeof(float) * (c->A + 1) * (c->F + 4);
+        HIP_TRY(allow_dynamic_lds((const void *)hp_kernels[k], lds, hp_lds_set[k]));
+        STAGE("heads_fwd", 2.0 * B * c->F * (c->A + 1), 4.0 * fc_nz * B * c->F);
+        // A block per compute unit at most.  With eight chunks or fewer (1024 units from 193 frames on) there is little to share out:
+        // calls of 193 / 224 / 256 frames of the stride-1 member 237 / 253 / 271 us with four frames a block, 233 / 250 / 269 with one.
+        if (B <= 256 && hf == LOADS_VEC16) {
+            static const HeadsPredict few[3] = {heads_predict_few_kernel<1>, heads_predict_few_kernel<2>, heads_predict_few_kernel<4>};
+            ga3c::launch(few[nj / 2], dim3(B), dim3(256), 0, s, fc_ws, fc_nz, fc_bias, B, c->A, th + c->off[nb + 2],
+                         th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5], logits, values, probs, uniforms, actions, c->rb);
+            HIP_TRY(hipGetLastError());
+            return GA3C_OK;
+        }
+        ga3c::launch(hp_kernels[k], dim3(cdiv(B, 4)), dim3(256), lds, s, fc_ws, fc_nz, fc_bias, B, c->A, th + c->off[nb + 2],
+                     th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5], logits, values, probs, uniforms, actions, c->rb);
+        HIP_TRY(hipGetLastError());
+        return GA3C_OK;
+    }
+    const size_t hf_lds = sizeof(float) * heads_lds_floats(c->F, c->A);
+    typedef decltype(&heads_fwd_kernel<LOADS_SCALAR>) HeadsFwd;
+    static const HeadsFwd hf_kernels[3] = {heads_fwd_kernel<LOADS_SCALAR>, heads_fwd_kernel<LOADS_VEC8>, heads_fwd_kernel<LOADS_VEC16>};
+    static size_t hf_lds_set[3] = {0, 0, 0};
+    HIP_TRY(allow_dynamic_lds((const void *)hf_kernels[hf], hf_lds, hf_lds_set[hf]));
+    STAGE("heads_fwd", 2.0 * B * c->F * (c->A + 1), 4.0 * (fc_nz + 1) * B * c->F);
+    ga3c::launch(hf_kernels[hf], dim3(cdiv(B, 4)), dim3(256), hf_lds, s, fc_ws, fc_nz,
+                       fc_bias, w.h, B, c->F, c->A, th + c->off[nb + 2],
+                       th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5],
+                       keep_zv ? w.zv : nullptr, logits, values, probs, uniforms, actions, c->rb, FastDiv(std::max(1, c->F / 4)), FastDiv(c->A + 1));
+    HIP_TRY(hipGetLastError());
+    return GA3C_OK;
 }
 
 // Forward pass of `B` frames into `w`; heads outputs to the optional pointers.  table (frames is nullptr then): the frames lie
@@ -2369,43 +2433,98 @@ int forward(ga3c_ctx *c, int which, Work &w, const uint8_t *frames, const uint8_
     }
     w.fc_ws = fc_ws; w.fc_nz = fc_nz;
     if (!with_heads) return GA3C_OK;          // the caller finishes the fc layer and the heads itself
-    const int hf = heads_loads(c->F, fc_nz, fc_ws, th + c->off[nb + 1], w.h, th + c->off[nb + 2]);
-    const int nj = c->F % 256 == 0 ? c->F / 256 : 0;
-    if (c->fast && !keep_zv && hf != LOADS_SCALAR && (nj == 1 || nj == 2 || nj == 4)) {
-        typedef decltype(&heads_predict_kernel<1, 8>) HeadsPredict;
-        static const HeadsPredict hp_kernels[6] = {heads_predict_kernel<1, 8>, heads_predict_kernel<1, 20>, heads_predict_kernel<2, 8>,
-                                                   heads_predict_kernel<2, 16>, heads_predict_kernel<4, 8>, heads_predict_kernel<4, 8>};
-        static size_t hp_lds_set[6] = {0, 0, 0, 0, 0, 0};
-        const int k = (nj == 1 ? 0 : nj == 2 ? 2 : 4) + (hf == LOADS_VEC16 ? 1 : 0);
-        const size_t lds = sizeof(float) * (c->A + 1) * (c->F + 4);
-        HIP_TRY(allow_dynamic_lds((const void *)hp_kernels[k], lds, hp_lds_set[k]));
-        STAGE("heads_fwd", 2.0 * B * c->F * (c->A + 1), 4.0 * fc_nz * B * c->F);
-        // A block per compute unit at most.  With eight chunks or fewer (1024 units from 193 frames on) there is little to share out:
-        // calls of 193 / 224 / 256 frames of the stride-1 member 237 / 253 / 271 us with four frames a block, 233 / 250 / 269 with one.
-        if (B <= 256 && hf == LOADS_VEC16) {
-            static const HeadsPredict few[3] = {heads_predict_few_kernel<1>, heads_predict_few_kernel<2>, heads_predict_few_kernel<4>};
-            ga3c::launch(few[nj / 2], dim3(B), dim3(256), 0, s, fc_ws, fc_nz, th + c->off[nb + 1], B, c->A, th + c->off[nb + 2],
-                         th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5], logits, values, probs, uniforms, actions, c->rb);
-            HIP_TRY(hipGetLastError());
-            return GA3C_OK;
-        }
-        ga3c::launch(hp_kernels[k], dim3(cdiv(B, 4)), dim3(256), lds, s, fc_ws, fc_nz, th + c->off[nb + 1], B, c->A, th + c->off[nb + 2],
-                     th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5], logits, values, probs, uniforms, actions, c->rb);
-        HIP_TRY(hipGetLastError());
-        return GA3C_OK;
+    return run_heads(c, which, w, fc_ws, fc_nz, th + c->off[nb + 1], B, keep_zv, logits, values, probs, uniforms, actions, s);
+}
+
+// --------------------------------------------------------- memory between the fc layer and the heads --
+//
+// The fc output behind its rectifier, x [B][F], is [queries | keys | values] of the memory's heads; attention with a decay reads out
+// of the agent's state, group norm (a group per head) and a rectifier follow, and the heads take x with that added to the values.
+
+ga3c_decay_desc memory_attention(const ga3c_ctx *c) {
+    const ga3c_memory_desc &m = c->memory;
+    return ga3c_decay_desc{m.heads, m.key_dim, m.value_dim, GA3C_F32, m.decay, m.heads ? 1.f / sqrtf((float)m.key_dim) : 0.f};
+}
+ga3c_norm_desc memory_norm(const ga3c_ctx *c) {
+    return ga3c_norm_desc{c->memory.heads * c->memory.value_dim, c->memory.heads, GA3C_F32, GA3C_ACT_RELU, 1e-5f};
+}
+// The heads' slices of x (or of its gradient), and what is read out of the memory (or its gradient).
+struct MemoryViews {
+    ga3c_heads q, k, v, out;
+    MemoryViews(const ga3c_ctx *c, float *x, float *o) {
+        const ga3c_memory_desc &m = c->memory;
+        q = {x, c->F, m.key_dim};
+        k = {x + m.heads * m.key_dim, c->F, m.key_dim};
+        v = {x + 2 * m.heads * m.key_dim, c->F, m.value_dim};
+        out = {o, m.heads * m.value_dim, m.value_dim};
     }
-    const size_t hf_lds = sizeof(float) * heads_lds_floats(c->F, c->A);
-    typedef decltype(&heads_fwd_kernel<LOADS_SCALAR>) HeadsFwd;
-    static const HeadsFwd hf_kernels[3] = {heads_fwd_kernel<LOADS_SCALAR>, heads_fwd_kernel<LOADS_VEC8>, heads_fwd_kernel<LOADS_VEC16>};
-    static size_t hf_lds_set[3] = {0, 0, 0};
-    HIP_TRY(allow_dynamic_lds((const void *)hf_kernels[hf], hf_lds, hf_lds_set[hf]));
-    STAGE("heads_fwd", 2.0 * B * c->F * (c->A + 1), 4.0 * (fc_nz + 1) * B * c->F);
-    ga3c::launch(hf_kernels[hf], dim3(cdiv(B, 4)), dim3(256), hf_lds, s, fc_ws, fc_nz,
-                       th + c->off[nb + 1], w.h, B, c->F, c->A, th + c->off[nb + 2],
-                       th + c->off[nb + 3], th + c->off[nb + 4], th + c->off[nb + 5],
-                       keep_zv ? w.zv : nullptr, logits, values, probs, uniforms, actions, c->rb, FastDiv(std::max(1, c->F / 4)), FastDiv(c->A + 1));
+};
+struct MemoryStep { const int32_t *agents; const uint8_t *starts; float *states; int n_agents; };
+
+// x from the fc layer's partial sums.
+__global__ __launch_bounds__(256) void memory_features_kernel(const float *__restrict__ ws, int nz, const float *__restrict__ bias, int n, int F, float *__restrict__ x) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    float s = bias[i % F];
+    for (int z = 0; z < nz; z += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = ws[(size_t)min(z + k, nz - 1) * n + i];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += z + k < nz ? v[k] : 0.f;
+    }
+    x[i] = s > 0.f ? s : 0.f;
+}
+int memory_features(ga3c_ctx *c, int which, Work &w, int B, hipStream_t s) {
+    STAGE("memory_features", 0, 4.0 * (w.fc_nz + 1) * B * c->F);
+    ga3c::launch(memory_features_kernel, dim3(cdiv(B * c->F, 256)), dim3(256), 0, s, w.fc_ws, w.fc_nz, c->theta2[which] + c->off[2 * c->nconv + 1], B * c->F, c->F, w.features(c->F));
     HIP_TRY(hipGetLastError());
     return GA3C_OK;
+}
+// What goes beside x into the heads.
+int memory_read_out(ga3c_ctx *c, int which, Work &w, int B, float *stats, hipStream_t s) {
+    STAGE("memory_norm", 0, 0);
+    const ga3c_norm_desc d = memory_norm(c);
+    const float *th = c->theta2[which];
+    return ga3c_group_norm(&d, w.mem_o, d.channels, th + c->off_gamma, th + c->off_beta, w.read_out(c->F, B) + c->F - d.channels, c->F, stats, B, 1,
+                           nullptr, 0, s);
+}
+// Frames that an episode begins with inside a segment: those behind one that ended.
+__global__ __launch_bounds__(256) void memory_starts_kernel(const uint8_t *__restrict__ dones, const int32_t *__restrict__ seg_start, int N, int T, int B, uint8_t *__restrict__ starts) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= B) return;
+    bool first = i == 0;
+    if (!seg_start) first = i % T == 0;
+    else {
+        int lo = 0, hi = N + 1;                         // the last entry that is not above i
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (seg_start[mid] <= i) lo = mid;
+            else hi = mid;
+        }
+        first = first || seg_start[lo] == i;
+    }
+    starts[i] = !first && dones[i - 1] != 0;
+}
+// dL/d(pre-activation of fc) = [x > 0] (what came through the heads + what came through the memory), and each block's sums over its
+// frames, as heads_dgrad_kernel leaves them.
+__global__ __launch_bounds__(HD_COLS) void memory_dgrad_kernel(const float *__restrict__ x, const float *__restrict__ dm, int B, int F, float *__restrict__ dh,
+                                                               float *__restrict__ colpart) {
+    const int k = blockIdx.y * HD_COLS + threadIdx.x, b0 = blockIdx.x * HD_FRAMES, nf = min(HD_FRAMES, B - b0);
+    if (k >= F) return;
+    float v[HD_FRAMES], col = 0.f;
+#pragma unroll
+    for (int f = 0; f < HD_FRAMES; ++f) {
+        const size_t i = (size_t)(b0 + min(f, nf - 1)) * F + k;
+        v[f] = x[i] > 0.f ? dh[i] + dm[i] : 0.f;
+    }
+#pragma unroll
+    for (int f = 0; f < HD_FRAMES; ++f)
+        if (f < nf) {
+            dh[(size_t)(b0 + f) * F + k] = v[f];
+            col += v[f];
+        }
+    colpart[(size_t)blockIdx.x * F + k] = col;
 }
 
 // Partial weight gradients that an update of B frames leaves for a layer on conv_band_grads.hpp's kernels; 0 for every other layer.
@@ -2475,6 +2594,9 @@ static int init_shape(ga3c_ctx *c, const ga3c_net_desc *d) {
     c->flat = C * H * W;
     c->off[no++] = pos; pos += (int64_t)c->flat * c->F;
     c->off[no++] = pos; pos += c->F;
+    const int read_out = c->memory.heads * c->memory.value_dim;
+    c->off_gamma = pos; pos += read_out;
+    c->off_beta = pos; pos += read_out;
     c->off[no++] = pos; pos += (int64_t)c->A * c->F;
     c->off[no++] = pos; pos += c->A;
     c->off[no++] = pos; pos += c->F;
@@ -2486,7 +2608,7 @@ static int init_shape(ga3c_ctx *c, const ga3c_net_desc *d) {
 
 // ------------------------------------------------------------------ C ABI ---
 
-extern "C" int ga3c_create(const ga3c_net_desc *d, int max_predict_batch, int max_train_frames, ga3c_ctx **out) {
+static int create(const ga3c_net_desc *d, const ga3c_memory_desc *memory, int max_predict_batch, int max_train_frames, ga3c_ctx **out) {
     if (out) *out = nullptr;
     if (!d || !out) return fail(GA3C_EINVAL, "ga3c_create: null argument");
     if (d->n_conv < 1 || d->n_conv > GA3C_MAX_CONV) return fail(GA3C_EINVAL, "ga3c_create: n_conv must be 1..4");
@@ -2504,6 +2626,7 @@ extern "C" int ga3c_create(const ga3c_net_desc *d, int max_predict_batch, int ma
     c->prof = new (std::nothrow) Profiler();
     c->fast = true;
     c->max_pred = max_predict_batch; c->max_train = max_train_frames;
+    if (memory) c->memory = *memory;
 
     if (init_shape(c, d) != GA3C_OK) {
         const int l = c->nconv;      // init_shape leaves the index of the offending layer here
@@ -2620,6 +2743,24 @@ extern "C" int ga3c_create(const ga3c_net_desc *d, int max_predict_batch, int ma
             if (e != hipSuccess) guard(fail(GA3C_EHIP, "hipMemset: %s", hipGetErrorString(e)));
         }
     }
+    if (rc == GA3C_OK && memory) {
+        guard(dmalloc((void **)&c->no_bias, sizeof(float) * c->F));
+        if (rc == GA3C_OK) {
+            const hipError_t e = hipMemset(c->no_bias, 0, sizeof(float) * c->F);
+            if (e != hipSuccess) guard(fail(GA3C_EHIP, "hipMemset: %s", hipGetErrorString(e)));
+        }
+        if (rc == GA3C_OK && max_train_frames > 0) {
+            const size_t frames = max_train_frames, read_out = (size_t)memory->heads * memory->value_dim;
+            guard(dmalloc((void **)&c->mem_stats, sizeof(float) * 2 * frames * memory->heads));
+            if (rc == GA3C_OK) guard(dmalloc((void **)&c->mem_do, sizeof(float) * frames * read_out));
+            if (rc == GA3C_OK) guard(dmalloc((void **)&c->mem_dm, sizeof(float) * frames * c->F));
+            if (rc == GA3C_OK) guard(dmalloc((void **)&c->mem_starts, frames));
+            const ga3c_decay_desc dd = memory_attention(c);
+            const ga3c_norm_desc nd = memory_norm(c);
+            c->mem_ws_bytes = std::max(ga3c_group_norm_workspace(&nd, max_train_frames, 1, 1), decay_workspace_most(&dd, max_train_frames));
+            if (rc == GA3C_OK) guard(dmalloc(&c->mem_ws, c->mem_ws_bytes));
+        }
+    }
     if (rc == GA3C_OK) guard(alloc_work(c->pred, c, max_predict_batch, false));
     if (rc == GA3C_OK) guard(alloc_work(c->train, c, max_train_frames, true));
     if (rc == GA3C_OK && max_train_frames > 0) {
@@ -2663,6 +2804,24 @@ extern "C" int ga3c_create(const ga3c_net_desc *d, int max_predict_batch, int ma
     return GA3C_OK;
 }
 
+extern "C" int ga3c_create(const ga3c_net_desc *d, int max_predict_batch, int max_train_frames, ga3c_ctx **out) {
+    return create(d, nullptr, max_predict_batch, max_train_frames, out);
+}
+
+extern "C" int ga3c_create_memory(const ga3c_net_desc *d, const ga3c_memory_desc *m, int max_predict_batch, int max_train_frames, ga3c_ctx **out) {
+    if (out) *out = nullptr;
+    if (!d || !m) return fail(GA3C_EINVAL, "ga3c_create_memory: null argument");
+    if (m->heads < 1 || m->heads > GA3C_MAX_MEMORY_HEADS) return fail(GA3C_EINVAL, "ga3c_create_memory: heads must be 1..%d", GA3C_MAX_MEMORY_HEADS);
+    for (int n : {m->key_dim, m->value_dim})
+        if (n < 1 || n > GA3C_MAX_HEAD_DIM) return fail(GA3C_EINVAL, "ga3c_create_memory: key_dim and value_dim must be 1..%d", GA3C_MAX_HEAD_DIM);
+    if (m->heads * (2 * m->key_dim + m->value_dim) != d->fc_units)
+        return fail(GA3C_EINVAL, "ga3c_create_memory: heads * (2 key_dim + value_dim) = %d, but fc_units = %d", m->heads * (2 * m->key_dim + m->value_dim), d->fc_units);
+    for (int h = 0; h < m->heads; ++h)
+        if (!(m->decay[h] >= 0.f && m->decay[h] <= 1.f)) return fail(GA3C_EINVAL, "ga3c_create_memory: decay of head %d outside [0, 1]", h);
+    if (d->math != 0) return fail(GA3C_EINVAL, "ga3c_create_memory: math must be 0");
+    return create(d, m, max_predict_batch, max_train_frames, out);
+}
+
 extern "C" int ga3c_destroy(ga3c_ctx *c) {
     if (!c) return GA3C_OK;
     (void)hipDeviceSynchronize();
@@ -2675,6 +2834,8 @@ extern "C" int ga3c_destroy(ga3c_ctx *c) {
     (void)hipFree(c->bfrag[0]); (void)hipFree(c->bfrag[1]); (void)hipFree(c->fcw[0].w);      // both copies' in one piece
     free_work(c->pred); free_work(c->train);
     (void)hipFree(c->dhp.w); (void)hipFree(c->dh); (void)hipFree(c->dzv); (void)hipFree(c->R);
+    (void)hipFree(c->no_bias); (void)hipFree(c->mem_stats); (void)hipFree(c->mem_do); (void)hipFree(c->mem_dm); (void)hipFree(c->mem_starts);
+    (void)hipFree(c->mem_ws);
     (void)hipFree(c->partials); (void)hipFree(c->colpart); (void)hipFree(c->scale); (void)hipFree(c->stats);
     if (c->prof) {
         for (ProfRec &r : c->prof->recs) { (void)hipEventDestroy(r.a); (void)hipEventDestroy(r.b); }
@@ -2688,9 +2849,11 @@ extern "C" int ga3c_destroy(ga3c_ctx *c) {
 extern "C" size_t ga3c_params_count(const ga3c_ctx *c) { return c ? c->P : 0; }
 
 extern "C" int ga3c_params_offsets(const ga3c_ctx *c, int64_t *off, int cap) {
-    if (!c || !off || cap < c->noff) return fail(GA3C_EINVAL, "ga3c_params_offsets: null argument or cap too small");
+    const int more = c && c->memory.heads ? 2 : 0;
+    if (!c || !off || cap < c->noff + more) return fail(GA3C_EINVAL, "ga3c_params_offsets: null argument or cap too small");
     for (int i = 0; i < c->noff; ++i) off[i] = c->off[i];
-    return c->noff;
+    if (more) { off[c->noff] = c->off_gamma; off[c->noff + 1] = c->off_beta; }
+    return c->noff + more;
 }
 
 extern "C" int ga3c_params_init(ga3c_ctx *c, uint64_t seed, void *stream) {
@@ -2704,6 +2867,10 @@ extern "C" int ga3c_params_init(ga3c_ctx *c, uint64_t seed, void *stream) {
     ga3c::launch(fill_kernel, dim3(blocks_for(c->P)), dim3(256), 0, s, c->g, c->P, 0.f);
     HIP_TRY(hipGetLastError());
     const int nb = 2 * c->nconv;
+    if (const size_t n = (size_t)c->memory.heads * c->memory.value_dim) {
+        ga3c::launch(fill_kernel, dim3(blocks_for(n)), dim3(256), 0, s, theta + c->off_gamma, n, 1.f);
+        HIP_TRY(hipGetLastError());
+    }
     // weight tensors and their fan-in; biases stay zero
     struct { int64_t off; size_t n; int fan_in; } t[GA3C_MAX_CONV + 3];
     int nt = 0;
@@ -2760,8 +2927,9 @@ extern "C" int ga3c_params_set(ga3c_ctx *c, int which, const float *src, size_t 
 }
 
 static int predict_impl(ga3c_ctx *c, const uint8_t *frames, const uint8_t *const *table, int B, const float *uniforms, float *logits,
-                        float *values, float *probs, int32_t *actions, void *stream) {
+                        float *values, float *probs, int32_t *actions, void *stream, const MemoryStep *memory = nullptr) {
     if (!c) return fail(GA3C_EINVAL, "ga3c_predict: null context");
+    if (!memory != !c->memory.heads) return fail(GA3C_EINVAL, c->memory.heads ? "ga3c_predict: the network has a memory (ga3c_predict_memory)" : "ga3c_predict_memory: the network has no memory");
     if (B < 0 || B > c->max_pred) return fail(GA3C_EINVAL, "ga3c_predict: B = %d outside [0, %d]", B, c->max_pred);
     if (B == 0) return GA3C_OK;
     if (!frames && !table) return fail(GA3C_EINVAL, "ga3c_predict: null frames");
@@ -2769,7 +2937,26 @@ static int predict_impl(ga3c_ctx *c, const uint8_t *frames, const uint8_t *const
     hipStream_t s = (hipStream_t)stream;
     TRY(wait_ready(c, s));
     TRY(begin_prediction(c, s));
-    return forward(c, c->cur, c->pred, frames, table, B, false, logits, values, probs, uniforms, actions, s);
+    if (!memory) return forward(c, c->cur, c->pred, frames, table, B, false, logits, values, probs, uniforms, actions, s);
+    Work &w = c->pred;
+    TRY(forward(c, c->cur, w, frames, table, B, false, nullptr, nullptr, nullptr, nullptr, nullptr, s, false));
+    TRY(memory_features(c, c->cur, w, B, s));
+    {
+        STAGE("memory_fwd", 4.0 * B * c->memory.heads * c->memory.key_dim * c->memory.value_dim, 0);
+        const ga3c_decay_desc d = memory_attention(c);
+        const MemoryViews v(c, w.features(c->F), w.mem_o);
+        TRY(ga3c_decay_attention_step(&d, &v.q, &v.k, &v.v, &v.out, memory->agents, memory->starts, B, memory->states, memory->n_agents, s));
+    }
+    TRY(memory_read_out(c, c->cur, w, B, nullptr, s));
+    return run_heads(c, c->cur, w, w.read_out(c->F, B), 2, c->no_bias, B, false, logits, values, probs, uniforms, actions, s);
+}
+
+extern "C" int ga3c_predict_memory(ga3c_ctx *c, const uint8_t *frames, int B, const int32_t *agents, const uint8_t *starts, float *states, int n_agents,
+                                   const float *uniforms, float *logits, float *values, float *probs, int32_t *actions, void *stream) {
+    if (B > 0 && !states) return fail(GA3C_EINVAL, "ga3c_predict_memory: null states");
+    if (n_agents < 0 || (!agents && B > n_agents)) return fail(GA3C_EINVAL, "ga3c_predict_memory: %d frames for %d states", B, n_agents);
+    const MemoryStep m{agents, starts, states, n_agents};
+    return predict_impl(c, frames, nullptr, B, uniforms, logits, values, probs, actions, stream, &m);
 }
 
 extern "C" int ga3c_predict(ga3c_ctx *c, const uint8_t *frames, int B, const float *uniforms, float *logits,
@@ -2781,7 +2968,7 @@ extern "C" int ga3c_predict(ga3c_ctx *c, const uint8_t *frames, int B, const flo
 // (B = N*T); otherwise N segments of unequal length, T = 1.
 static int train_step_impl(ga3c_ctx *c, const uint8_t *frames, const uint8_t *const *table, const int32_t *actions, const float *rewards,
                            const uint8_t *dones, const float *bootstrap, const int32_t *seg_start, int N, int T, int B,
-                           const ga3c_hparams *hp, ga3c_train_stats *stats, void *stream) {
+                           const ga3c_hparams *hp, ga3c_train_stats *stats, void *stream, const float *states = nullptr) {
     hipStream_t s = (hipStream_t)stream;
     Work &w = c->train;
     const int nb = 2 * c->nconv, A = c->A, F = c->F;
@@ -2795,9 +2982,24 @@ static int train_step_impl(ga3c_ctx *c, const uint8_t *frames, const uint8_t *co
     // update, separate kernels / this one, small net with 32 actions 40 frames 85.7 / 68.0, 2560 frames 304.7 / 292.7, with 63 actions
     // 104.0 / 72.1 and 330.1 / 302.1; larger net with 32 actions 640 frames 357.6 / 336.3.
     const size_t ht_lds = sizeof(float) * (size_t)heads_train_lds_floats(F, A);
-    const bool fused_heads = c->fast && ht_lds <= HEADS_TRAIN_MAX_LDS && A <= 31;
-    int rc = forward(c, cur, w, frames, table, B, true, nullptr, nullptr, nullptr, nullptr, nullptr, s, !fused_heads);
+    const bool memory = c->memory.heads > 0;
+    const bool fused_heads = c->fast && ht_lds <= HEADS_TRAIN_MAX_LDS && A <= 31 && !memory;
+    int rc = forward(c, cur, w, frames, table, B, true, nullptr, nullptr, nullptr, nullptr, nullptr, s, !fused_heads && !memory);
     if (rc != GA3C_OK) return rc;
+    const ga3c_decay_desc attention = memory_attention(c);
+    const ga3c_norm_desc norm = memory_norm(c);
+    if (memory) {
+        TRY(memory_features(c, cur, w, B, s));
+        {
+            STAGE("memory_fwd", 4.0 * B * c->memory.heads * c->memory.key_dim * c->memory.value_dim, 0);
+            ga3c::launch(memory_starts_kernel, dim3(cdiv(B, 256)), dim3(256), 0, s, dones, seg_start, N, T, B, c->mem_starts);
+            HIP_TRY(hipGetLastError());
+            const MemoryViews v(c, w.features(c->F), w.mem_o);
+            TRY(ga3c_decay_attention(&attention, &v.q, &v.k, &v.v, &v.out, seg_start, c->mem_starts, N, B, states, nullptr, c->mem_ws, c->mem_ws_bytes, s));
+        }
+        TRY(memory_read_out(c, cur, w, B, c->mem_stats, s));
+        TRY(run_heads(c, cur, w, w.read_out(F, B), 2, c->no_bias, B, true, nullptr, nullptr, nullptr, nullptr, nullptr, s));
+    }
 
     const int nloss = fused_heads ? cdiv(B, HD_FRAMES) : cdiv(B, LOSS_THREADS);
     float *losspart = c->partials + c->max_norm_parts;
@@ -2890,6 +3092,22 @@ static int train_step_impl(ga3c_ctx *c, const uint8_t *frames, const uint8_t *co
         ga3c::launch(heads_dgrad_kernel, dim3(cdiv(B, HD_FRAMES), cdiv(F, HD_COLS)), dim3(HD_COLS), hd_lds, s, c->dzv, w.h, Wp, Wv, B,
                            F, A, c->dh, c->colpart, (float *)nullptr, c->rb);
         HIP_TRY(hipGetLastError());
+    }
+    if (memory) {       // dh is the gradient of what goes into the heads: on through the memory, and to the fc layer's own rectifier
+        const int read_out = c->memory.heads * c->memory.value_dim;
+        float *dgamma = c->grad + c->off_gamma, *dbeta = c->grad + c->off_beta;
+        {
+            STAGE("memory_bwd", 10.0 * B * c->memory.heads * c->memory.key_dim * c->memory.value_dim, 0);
+            TRY(ga3c_group_norm_grad(&norm, w.mem_o, read_out, c->dh + F - read_out, F, th + c->off_gamma, th + c->off_beta, c->mem_stats, c->mem_do, read_out,
+                                     dgamma, dbeta, B, 1, c->mem_ws, c->mem_ws_bytes, s));
+            const MemoryViews v(c, w.features(F), c->mem_do), g(c, c->mem_dm, nullptr);
+            TRY(ga3c_decay_attention_grad(&attention, &v.q, &v.k, &v.v, &v.out, &g.q, &g.k, &g.v, seg_start, c->mem_starts, N, B, states, nullptr, nullptr,
+                                          c->mem_ws, c->mem_ws_bytes, s));
+            ga3c::launch(memory_dgrad_kernel, dim3(cdiv(B, HD_FRAMES), cdiv(F, HD_COLS)), dim3(HD_COLS), 0, s, w.features(F), c->mem_dm, B, F, c->dh, c->colpart);
+            HIP_TRY(hipGetLastError());
+        }
+        add_seg(dgamma, 1, 1, read_out, 0, 1, dgamma, nullptr, 0);      // whole already: for the gradient's norm
+        add_seg(dbeta, 1, 1, read_out, 0, 1, dbeta, nullptr, 0);
     }
     const float *xfc = w.act[c->nconv - 1];
     const float *wfc = th + c->off[nb];
@@ -3099,6 +3317,7 @@ extern "C" int ga3c_train_step(ga3c_ctx *c, const uint8_t *frames, const int32_t
     if (BL > c->max_train) return fail(GA3C_EINVAL, "ga3c_train_step: N*T = %lld above capacity %d", BL, c->max_train);
     if (BL == 0) return GA3C_OK;
     if (!frames || !actions || !rewards || !dones || !hp) return fail(GA3C_EINVAL, "ga3c_train_step: null argument");
+    if (c->memory.heads) return fail(GA3C_EINVAL, "ga3c_train_step: the network has a memory (ga3c_train_step_memory)");
     return train_step_impl(c, frames, nullptr, actions, rewards, dones, bootstrap, nullptr, N, T, (int)BL, hp, stats, stream);
 }
 
@@ -3113,8 +3332,25 @@ extern "C" int ga3c_train_step_ragged(ga3c_ctx *c, const uint8_t *frames, const 
     if (N == 0) return fail(GA3C_EINVAL, "ga3c_train_step_ragged: frames without a segment");
     if (!frames || !actions || !rewards || !dones || !seg_start || !hp)
         return fail(GA3C_EINVAL, "ga3c_train_step_ragged: null argument");
+    if (c->memory.heads) return fail(GA3C_EINVAL, "ga3c_train_step_ragged: the network has a memory (ga3c_train_step_memory)");
     return train_step_impl(c, frames, nullptr, actions, rewards, dones, bootstrap, seg_start, N, 1, n_frames, hp, stats, stream);
 }
+
+extern "C" int ga3c_train_step_memory(ga3c_ctx *c, const uint8_t *frames, const int32_t *actions, const float *rewards, const uint8_t *dones,
+                                      const int32_t *seg_start, const float *states, const float *bootstrap, int N, int n_frames,
+                                      const ga3c_hparams *hp, ga3c_train_stats *stats, void *stream) {
+    if (!c) return fail(GA3C_EINVAL, "ga3c_train_step_memory: null context");
+    if (!c->memory.heads) return fail(GA3C_EINVAL, "ga3c_train_step_memory: the network has no memory");
+    if (N < 0 || n_frames < 0) return fail(GA3C_EINVAL, "ga3c_train_step_memory: negative N or n_frames");
+    if (n_frames > c->max_train) return fail(GA3C_EINVAL, "ga3c_train_step_memory: %d frames above capacity %d", n_frames, c->max_train);
+    if (n_frames == 0) return GA3C_OK;
+    if (N == 0) return fail(GA3C_EINVAL, "ga3c_train_step_memory: frames without a segment");
+    if (!seg_start && n_frames % N) return fail(GA3C_EINVAL, "ga3c_train_step_memory: %d frames are no %d equal segments", n_frames, N);
+    if (!frames || !actions || !rewards || !dones || !hp) return fail(GA3C_EINVAL, "ga3c_train_step_memory: null argument");
+    return train_step_impl(c, frames, nullptr, actions, rewards, dones, bootstrap, seg_start, N, seg_start ? 1 : n_frames / N, n_frames, hp, stats, stream, states);
+}
+
+bool ga3c::has_memory(const ga3c_ctx *c) { return c->memory.heads > 0; }
 
 // What the scheduler calls (frame_table.hpp).
 bool ga3c::takes_frame_table(const ga3c_ctx *c) {

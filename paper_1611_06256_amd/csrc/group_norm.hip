@@ -691,18 +691,18 @@ int check_cut(const Cut &c, const char *who) {
 
 using namespace ga3c;
 
-extern "C" size_t ga3c_group_norm_workspace(const ga3c_norm_desc *d, int n_samples, int n_positions) {
+extern "C" size_t ga3c_group_norm_workspace(const ga3c_norm_desc *d, int n_samples, int n_positions, int grad) {
     if (check(d, n_samples, n_positions, "ga3c_group_norm_workspace") != GA3C_OK || n_samples == 0) return 0;
     size_t most = 0;
-    for (int i = 0; i < 4; ++i) {        // whether the tensors allow vectors is not known here
-        const Cut c = cut_of(d, n_samples, n_positions, i & 1, i & 2);
-        most = std::max(most, sums_floats(d, c, n_samples) + (i & 2 ? partial_floats(d, c) : 0));
+    for (bool vectors : {false, true}) {        // whether the tensors allow them is not known here
+        const Cut c = cut_of(d, n_samples, n_positions, vectors, grad != 0);
+        most = std::max(most, sums_floats(d, c, n_samples) + (grad ? partial_floats(d, c) : 0));
     }
     return sizeof(float) * most;
 }
 
-static int check_workspace(const ga3c_norm_desc *d, int samples, int positions, void *workspace, size_t bytes, const char *who) {
-    const size_t need = ga3c_group_norm_workspace(d, samples, positions);
+static int check_workspace(const ga3c_norm_desc *d, int samples, int positions, int grad, void *workspace, size_t bytes, const char *who) {
+    const size_t need = ga3c_group_norm_workspace(d, samples, positions, grad);
     if (bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
     return GA3C_OK;
@@ -718,7 +718,7 @@ extern "C" int ga3c_group_norm(const ga3c_norm_desc *d, const void *x, int64_t x
     if (!gamma || !beta) return call_fail(GA3C_EINVAL, "%s: null gamma or beta", who);
     if ((uintptr_t)stats % 8) return call_fail(GA3C_EINVAL, "%s: stats not aligned to 8 bytes", who);
     if (x == y) return call_fail(GA3C_EINVAL, "%s: the result is the input", who);
-    if ((rc = check_workspace(d, n_samples, n_positions, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
+    if ((rc = check_workspace(d, n_samples, n_positions, 0, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
     const Cut c = cut_of(d, n_samples, n_positions, whole_vectors(d, {x, y}, {x_stride, y_stride}, gamma, beta), false);
     if ((rc = check_cut(c, who)) != GA3C_OK) return rc;
     NormArgs a = args_of(d, c, n_samples, n_positions, workspace);
@@ -741,7 +741,7 @@ extern "C" int ga3c_group_norm_grad(const ga3c_norm_desc *d, const void *x, int6
         if (!gamma || !beta || !stats) return call_fail(GA3C_EINVAL, "%s: null gamma, beta or stats", who);
         if ((uintptr_t)stats % 8) return call_fail(GA3C_EINVAL, "%s: stats not aligned to 8 bytes", who);
         if (dx == x || dx == dy) return call_fail(GA3C_EINVAL, "%s: the result is an input", who);
-        if ((rc = check_workspace(d, n_samples, n_positions, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
+        if ((rc = check_workspace(d, n_samples, n_positions, 1, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
         c = cut_of(d, n_samples, n_positions, whole_vectors(d, {x, dy, dx}, {x_stride, dy_stride, dx_stride}, gamma, beta), true);
         if ((rc = check_cut(c, who)) != GA3C_OK) return rc;
     }

@@ -403,6 +403,7 @@ extern "C" int ga3c_sched_create(ga3c_ctx *ctx, const ga3c_sched_config *cfg, ga
     ga3c_net_desc d;
     int mp, mt;
     if (ga3c_get_desc(ctx, &d, &mp, &mt) != GA3C_OK) return sfail(GA3C_EINVAL, "ga3c_sched_create: bad context");
+    if (ga3c::has_memory(ctx)) return sfail(GA3C_EINVAL, "ga3c_sched_create: the queues take no networks with a memory");
     const size_t fb = (size_t)d.in_c * d.in_h * d.in_w;
     if (fb % 16 != 0) return sfail(GA3C_EINVAL, "ga3c_sched_create: frame size must be a multiple of 16 bytes");
     if (cfg->t_max < 1 || cfg->predict_cap < 1 || cfg->predict_cap > mp || cfg->train_min < 1 ||

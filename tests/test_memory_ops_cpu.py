@@ -37,7 +37,7 @@ def test_attention_refuses_bad_descriptions():
         assert forward(lib, desc(**kw), v) == -1 and text in lib.ga3c_last_error(), kw
         step = lib.ga3c_decay_attention_step(C.byref(desc(**kw)), *[C.byref(x) for x in v], None, None, 4, A, 8, None)
         assert step == -1 and text in lib.ga3c_last_error(), kw
-        assert lib.ga3c_decay_attention_workspace(C.byref(desc(**kw)), 2, 8) == 0
+        assert lib.ga3c_decay_attention_workspace(C.byref(desc(**kw)), 2, 8, 1) == 0
     assert lib.ga3c_decay_attention(None, *[C.byref(x) for x in v], None, None, 2, 8, None, None, None, 0, None) == -1
     no_decay = binding._DecayDesc(2, 16, 32, 0, None, 1.0)
     assert forward(lib, no_decay, v) == -1 and b"null" in lib.ga3c_last_error()
@@ -169,3 +169,30 @@ def test_reference_against_the_sum_over_tokens_and_differences():
         way = torch.randn_like(x[i])
         ends = [loss(*[y + e * way if j == i else y for j, y in enumerate(x)]) for e in (1e-5, -1e-5)]
         assert abs((ends[0] - ends[1]) / 2e-5 - float((gr * way).sum())) < 1e-6
+
+
+def test_networks_with_a_memory_are_checked():
+    lib = g.load_library()
+    ctx = C.c_void_p()
+    net = g.SMALL_NET(6).c()
+
+    def create(n=net, **kw):
+        m = binding._MemoryDesc(4, 16, 32, (C.c_float * 16)(0.5, 0.6, 0.7, 1.0))
+        for k, v in kw.items():
+            setattr(m, k, v)
+        return lib.ga3c_create_memory(C.byref(n) if n else None, C.byref(m), 1, 1, C.byref(ctx))
+
+    for kw, text in [(dict(heads=0), b"heads"), (dict(heads=17), b"heads"), (dict(key_dim=0), b"key_dim"), (dict(value_dim=129), b"key_dim"),
+                     (dict(heads=3), b"fc_units = 256"), (dict(decay=(C.c_float * 16)(0.5, 0.5, 2.0, 0.5)), b"decay of head 2"),
+                     (dict(decay=(C.c_float * 16)(float("nan"))), b"decay of head 0"), (dict(n=None), b"null")]:
+        assert create(**kw) == -1 and text in lib.ga3c_last_error() and not ctx.value, kw
+    net.math = 1
+    assert create() == -1 and b"math" in lib.ga3c_last_error()
+    assert lib.ga3c_predict_memory(None, A, 1, None, None, A, 1, None, None, None, None, None, None) == -1
+    assert lib.ga3c_predict_memory(None, A, 1, None, None, None, 1, None, None, None, None, None, None) == -1
+    assert lib.ga3c_predict_memory(None, A, 2, None, None, A, 1, None, None, None, None, None, None) == -1
+    hp = g.HParams().c()
+    assert lib.ga3c_train_step_memory(None, A, A, A, A, None, None, None, 1, 5, C.byref(hp), None, None) == -1
+    with pytest.raises(g.Ga3cError, match="decay"):
+        g.MemoryDesc(heads=3).c()
+    assert C.sizeof(binding._MemoryDesc) == 76 and C.sizeof(binding._DecayDesc) == 32 and C.sizeof(binding._NormDesc) == 20
