@@ -463,7 +463,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
 
     const bool vec_out = (uintptr_t)p.out.data % (4 * sizeof(T)) == 0 && ((p.out.token | p.out.head | rows) % 4) == 0;
     bool passes = true;                                             // whether the state in front of the span reaches its end
-    const bool mine = RP / 16 == WAVES || wave < RP / 16;
+    const bool mine = 16 * wave < rows;                             // the wavefront has rows
     const int along = IC::along_start(g, l16), fours = IC::fours_start(g, l16);
     const auto row_across = IR::across_start(g, l16);
     const auto col_across = IC::across_start(g, l16);

@@ -40,17 +40,21 @@ struct NormArgs {
     int chunk, chunks;               // positions of a chunk, and chunks of a sample
 };
 
+// 1 / (1 + exp(-z)) from the hardware's power of two and reciprocal, each within a unit in the last place; the exponent's rounding
+// moves the result by less than |z| 2^-24 of itself, at most 3 units where it counts.  (With the library's exponential and a full
+// division the arithmetic of 64 maps of bfloat16 took longer than their way from and to memory.)
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 template <int ACT>
 __device__ inline float activation(float z) {
     if (ACT == GA3C_ACT_RELU) return z > 0.f ? z : 0.f;
-    if (ACT == GA3C_ACT_SILU) return z / (1.f + expf(-z));
+    if (ACT == GA3C_ACT_SILU) return z * sigmoid(z);
     return z;
 }
 template <int ACT>
 __device__ inline float activation_slope(float z) {
     if (ACT == GA3C_ACT_RELU) return z > 0.f ? 1.f : 0.f;
     if (ACT == GA3C_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
+        const float s = sigmoid(z);
         return s * (1.f + z * (1.f - s));
     }
     return 1.f;
@@ -122,17 +126,19 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const NormArgs a, int lg
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
+        if (li + lg * j < a.per_group)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sum += li + lg * j < a.per_group ? in[j][e] : 0.f;
+            for (int e = 0; e < VE; ++e) sum += in[j][e];
     const float mean = lanes_sum(sum, lg) / (float)a.wide;
     sum = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
+        if (li + lg * j < a.per_group)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            const float d = in[j][e] - mean;
-            sum += li + lg * j < a.per_group ? d * d : 0.f;
-        }
+            for (int e = 0; e < VE; ++e) {
+                const float d = in[j][e] - mean;
+                sum += d * d;
+            }
     const float rstd = 1.f / sqrtf(lanes_sum(sum, lg) / (float)a.wide + a.eps);
     if (!there) return;
     T *y = (T *)a.y + sample * a.ys + group * a.wide;
@@ -180,15 +186,15 @@ __global__ __launch_bounds__(256) void norm_rows_grad_kernel(const NormArgs a, i
         float s = 0.f, sx = 0.f, xh[NV][VE], d[NV][VE];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const bool in_group = li + lg * j < a.per_group;
+            if (li + lg * j >= a.per_group) continue;
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 xh[j][e] = (in[j][e] - st.x) * st.y;
-                const float dz = in_group ? gr[j][e] * activation_slope<ACT>(xh[j][e] * g[j][e] + b[j][e]) : 0.f;
-                dg[j][e] += in_group ? dz * xh[j][e] : 0.f;
+                const float dz = gr[j][e] * activation_slope<ACT>(xh[j][e] * g[j][e] + b[j][e]);
+                dg[j][e] += dz * xh[j][e];
                 db[j][e] += dz;
                 d[j][e] = dz * g[j][e];
-                s += d[j][e]; sx += in_group ? d[j][e] * xh[j][e] : 0.f;
+                s += d[j][e]; sx += d[j][e] * xh[j][e];
             }
         }
         const float ma = lanes_sum(s, lg) / (float)a.wide, mb = lanes_sum(sx, lg) / (float)a.wide;
@@ -293,8 +299,9 @@ __global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
         float s = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
+            if (w.c >= 0 && w.row + w.rows * j < positions)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s += w.c >= 0 && w.row + w.rows * j < positions ? in[j][e] : 0.f;
+                for (int e = 0; e < VE; ++e) s += in[j][e];
         group_sums<NT>(a, w, groups, s, each, mean_of);
         const float mean = mean_of[w.group] / m;
         s = 0.f;
@@ -302,11 +309,12 @@ __global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
         for (int j = 0; j < NV; ++j) in[j].again();
 #pragma unroll
         for (int j = 0; j < NV; ++j)
+            if (w.c >= 0 && w.row + w.rows * j < positions)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float d = in[j][e] - mean;
-                s += w.c >= 0 && w.row + w.rows * j < positions ? d * d : 0.f;
-            }
+                for (int e = 0; e < VE; ++e) {
+                    const float d = in[j][e] - mean;
+                    s += d * d;
+                }
         group_sums<NT>(a, w, groups, s, each, rstd_of);
         if constexpr (MODE == CHUNK_SUMS) {
             for (int g = threadIdx.x; g < groups; g += NT)
@@ -369,16 +377,14 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             __builtin_amdgcn_sched_barrier(0);
-            const bool there = w.c >= 0 && row + w.rows * j < positions;
+            if (MODE == CHUNK_RESULT || w.c < 0 || row + w.rows * j >= positions) continue;
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float xh = (in[j][e] - st.x) * st.y, dz = gr[j][e] * activation_slope<ACT>(xh * g[e] + b[e]);
-                if (MODE != CHUNK_RESULT) {
-                    dg[e] += there ? dz * xh : 0.f;
-                    db[e] += there ? dz : 0.f;
-                    s += there ? dz * g[e] : 0.f;
-                    sx += there ? dz * g[e] * xh : 0.f;
-                }
+                const float xh = (in[j][e] - st.x) * st.y, dz = gr[j][e] * activation_slope<ACT>(xh * g[e] + b[e]), d = dz * g[e];
+                dg[e] += dz * xh;
+                db[e] += dz;
+                s += d;
+                sx += d * xh;
             }
         }
         if constexpr (MODE == CHUNK_RESULT) {
