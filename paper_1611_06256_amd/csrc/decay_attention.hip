@@ -463,7 +463,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
 
     const bool vec_out = (uintptr_t)p.out.data % (4 * sizeof(T)) == 0 && ((p.out.token | p.out.head | rows) % 4) == 0;
     bool passes = true;                                             // whether the state in front of the span reaches its end
-    const bool mine = 16 * wave < rows;                             // the wavefront has rows
+    const bool mine = MAIN ? 16 * wave < rows : RP / 16 == WAVES || wave < RP / 16;      // the wavefront has rows
     const int along = IC::along_start(g, l16), fours = IC::fours_start(g, l16);
     const auto row_across = IR::across_start(g, l16);
     const auto col_across = IC::across_start(g, l16);
@@ -605,7 +605,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                 }
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    if (MAIN && ct % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    if (ct % (MAIN ? 4 : 2) == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int k = 0; k < KT; ++k) {
                         colf = IC::across(now + L::COL, col_across, ct, k);
@@ -638,35 +638,42 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
 }
 
 // The states between the spans of a segment, from the segment's first state and what each span made of nothing: in place.
+// QUAD: four numbers per thread.
+template <bool QUAD>
 __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, int parts) {
+    typedef typename std::conditional<QUAD, f32x4, float>::type V;
     const DecayPass &p = job.pass[blockIdx.z / parts];
     const int seg = blockIdx.x, head = blockIdx.y, heads = gridDim.y;
     int first, end;
     segment_tokens(job, seg, first, end);
     const int spans = (end - first + job.span - 1) / job.span;
-    if (spans < 2 || end - first <= job.brief) return;
-    const int e = (blockIdx.z % parts) * 256 + threadIdx.x;
+    if (spans < 2) return;
+    const int e = ((blockIdx.z % parts) * 256 + threadIdx.x) * (QUAD ? 4 : 1);
     const size_t size = (size_t)p.rows * p.cols;
     if (e >= (int)size) return;
     const int item = job.seg_start ? first / job.span + seg : seg * (job.len / job.span + 1);
     float *at_span = p.spans + ((size_t)item * heads + head) * size + e;
     const float *passes = p.spans + (size_t)job.items * heads * size + (size_t)item * heads + head;
     const float w = (float)power((double)job.decay[head], job.span);
-    float x = p.x_in ? p.x_in[((size_t)seg * heads + head) * size + e] : 0.f;
+    V x{};
+    if (p.x_in) __builtin_memcpy(&x, p.x_in + ((size_t)seg * heads + head) * size + e, sizeof x);
     constexpr int AHEAD = 8;                              // spans whose numbers are under way together
     for (int i = 0; i + 1 < spans; i += AHEAD) {
-        float f[AHEAD], v[AHEAD];
+        float f[AHEAD];
+        V v[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const size_t at = (size_t)min(i + k, spans - 2) * heads;
-            f[k] = passes[at] * w;
-            v[k] = at_span[at * size];
+            f[k] = passes[at];
+            v[k] = *(const V *)(at_span + at * size);
         }
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            x = (f[k] == 0.f ? 0.f : f[k] * x) + v[k];
-            if (i + k + 1 < spans) at_span[(size_t)(i + k) * heads * size] = x;
-        }
+        for (int k = 0; k < AHEAD; ++k)
+            if (i + k + 1 < spans) {
+                if (f[k] == 0.f || w == 0.f) x = V{};     // whatever was in it
+                x = w * x + v[k];
+                *(V *)(at_span + (size_t)(i + k) * heads * size) = x;
+            }
     }
 }
 
@@ -871,19 +878,30 @@ hipError_t by_sizes(const DecayJob &job, int passes, F go) {
     return hipSuccess;
 }
 
-// Tokens that a block of the chunked kernels takes.  Spans of a segment cost its keys and values read twice and two states each,
-// so there are no more of them than it takes to give every compute unit a block.
-constexpr int SHORTEST_SPAN = 256;
-int span_of(int heads, int n_tokens) {
-    const int64_t want = (int64_t)n_tokens * heads / 256;
-    return (int)std::min<int64_t>(1 << 20, std::max<int64_t>(SHORTEST_SPAN, (want + 63) / 64 * 64));
+// Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN.  Longer spans leave compute units
+// idle or wait for one another at the end, shorter ones begin more often (about three tiles' time) and leave more states behind.
+// Counted in tiles, with two blocks per compute unit if both sizes are above 64 and one if not.  Measured against twice and half of
+// what it picks, us of the kernels: 16384 tokens bf16, 8 heads of 128 (512): 84 / 93 and 101; 24 episodes of 6001 tokens fp32, 6 heads of
+// 48 and 80 (128): 59 / 94 with 256; gradient of 4096 tokens fp32, 4 heads of 128 (256): 98 / 112 with 128.
+constexpr int SHORTEST_SPAN = 128;
+int span_of(int heads, int n_segments, int n_tokens, int key, int value, int passes, bool bf) {
+    const int tile = bf ? Tile<bf16>::C : Tile<float>::C;
+    const int64_t slots = key > 64 && value > 64 ? 256 : 512;
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int span = SHORTEST_SPAN; span <= 1 << 20; span *= 2) {
+        const int64_t blocks = (n_tokens / span + n_segments / 2) * (int64_t)heads * passes;      // half of a segment's last span is not there
+        const int64_t time = std::max<int64_t>(1, (blocks + slots - 1) / slots) * (std::min(span, n_tokens) / tile + 3);
+        if (time < least) { least = time; best = span; }
+    }
+    return best;
 }
 // Segments of up to so many tokens take the token-by-token kernel if the average is short.
 constexpr int BRIEF = 32;
 
-void plan(DecayJob &job, int heads) {
+void plan(DecayJob &job, const ga3c_decay_desc *d, bool grad) {
     job.brief = job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
-    job.span = job.brief >= 0 ? 1 << 30 : span_of(heads, job.n_tokens);
+    job.span = job.brief >= 0 ? 1 << 30 : span_of(d->n_heads, job.n_segments, job.n_tokens, d->key_dim, d->value_dim, grad ? 3 : 1, d->dtype == GA3C_BF16);
     job.items = job.brief >= 0 ? job.n_tokens / (job.brief + 1) + 1
                                : job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
 }
@@ -905,8 +923,11 @@ hipError_t run_job(DecayJob &job, int passes, const int *sources, int n_sources,
         for (int i = 0; i < n_sources; ++i) made.pass[i] = job.pass[sources[i]];
         e = by_sizes(made, n_sources, [&](const DecayJob &some, int n) { return launch_chunk<T, false>(some, n, heads, s); });
         if (e != hipSuccess) return e;
-        const int parts = (job.pass[0].rows * job.pass[0].cols + 255) / 256;
-        launch(decay_spans_kernel, dim3(job.n_segments, heads, parts * n_sources), dim3(256), 0, s, made, parts);
+        // four numbers per thread where that leaves enough blocks (one segment of 16384 tokens: 10 us, with four 16)
+        const int size = job.pass[0].rows * job.pass[0].cols;
+        const bool quad = size % 4 == 0 && (int64_t)job.n_segments * heads * n_sources * size >= 1 << 20;
+        const int each = quad ? 1024 : 256, parts = (size + each - 1) / each;
+        launch(quad ? decay_spans_kernel<true> : decay_spans_kernel<false>, dim3(job.n_segments, heads, parts * n_sources), dim3(256), 0, s, made, parts);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_chunk<T, true>(some, n, heads, s); });
@@ -961,13 +982,13 @@ bool overlap(const void *a, const void *b, size_t bytes) {
 }
 DecayView view(const ga3c_heads *h) { return h ? DecayView{h->data, h->token_stride, h->head_stride} : DecayView{nullptr, 0, 0}; }
 
-DecayJob job_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_t *starts, int n_segments, int n_tokens) {
+DecayJob job_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_t *starts, int n_segments, int n_tokens, bool grad) {
     DecayJob j;
     memset(&j, 0, sizeof j);
     j.seg_start = seg_start; j.starts = starts; j.n_segments = n_segments; j.n_tokens = n_tokens;
     j.len = n_tokens / n_segments;
     memcpy(j.decay, d->decay, sizeof(float) * d->n_heads);
-    plan(j, d->n_heads);
+    plan(j, d, grad);
     return j;
 }
 DecayPass pass_of(const ga3c_heads *row, const ga3c_heads *col, const ga3c_heads *by, const ga3c_heads *out, int rows, int cols, int turned, int back,
@@ -987,7 +1008,7 @@ using namespace ga3c;
 extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n_segments, int n_tokens, int grad) {
     if (check_desc(d, "ga3c_decay_attention_workspace") != GA3C_OK || n_segments < 1 || n_tokens < 1) return 0;
     // as with a table, which needs the most; the gradient has states of both directions
-    const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens);
+    const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens, grad);
     return (grad ? 2 : 1) * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
 }
 
@@ -1016,7 +1037,7 @@ extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *
     const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens, 0);
     if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
-    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);
+    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens, false);
     j.pass[0] = pass_of(v, k, q, out, d->value_dim, d->key_dim, 0, 0, d->scale, 1.f, state_in, state_out, (float *)workspace);
     const int sources[] = {0};
     return hip_result(run(d, j, 1, sources, 1, (hipStream_t)stream), who);
@@ -1041,7 +1062,7 @@ extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_he
     const size_t need = ga3c_decay_attention_workspace(d, n_segments, n_tokens, 1);
     if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
-    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens);
+    DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens, true);
     const int key = d->key_dim, value = d->value_dim;
     float *forward = (float *)workspace, *backward = forward + spans_floats(j, d->n_heads, (size_t)key * value);
     // the states in front of the tokens once more, read out by dout; the gradient of the state behind each token, read out by v and k
