@@ -178,7 +178,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // A fragment is 16 bytes of one lane: KB numbers of the contraction in the wavefront, VE of them in the lane.
 template <class T> struct Tile;
 template <> struct Tile<float> {
-    static constexpr int C = 32, KB = 16, VE = 4, TERMS = 1;
+    static constexpr int KB = 16, VE = 4, TERMS = 1;
     typedef f32x4 Frag;
     typedef f32x4 Quad;
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -189,7 +189,7 @@ template <> struct Tile<float> {
     __device__ static Quad quad(f32x4 v) { return v; }
 };
 template <> struct Tile<bf16> {
-    static constexpr int C = 64, KB = 32, VE = 8, TERMS = 3;
+    static constexpr int KB = 32, VE = 8, TERMS = 3;
     typedef bf16x8 Frag;
     typedef bf16x4 Quad;
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -200,10 +200,10 @@ template <> struct Tile<bf16> {
 // reading reach all banks: the same piece of sixteen rows, and (16 bits) two neighbouring pieces of rows 0-3, 8-11, 16-19, 24-27,
 // (32 bits) four pieces of every fourth row.  The order is an exclusive or, so a lane's place in one step of a contraction gives
 // the others with one instruction each: `start` is the lane's, the rest is the same for all lanes.
-template <class T, int D>
+template <class T, int C, int D>
 struct Image {
     typedef Tile<T> W;
-    static constexpr int PIECES = D * (int)sizeof(T) / 16, ROW = 16 * PIECES, BYTES = W::C * ROW;
+    static constexpr int PIECES = D * (int)sizeof(T) / 16, ROW = 16 * PIECES, BYTES = C * ROW;
     __device__ static int order(int row) {
         if (sizeof(T) == 4) return row & 15;
         if (PIECES >= 16) return (row >> 2 & 1) | (row & 3) << 1 | (row & 8);
@@ -249,13 +249,20 @@ struct Image {
     }
 };
 
+// Positions of a tile, C.  With 16 bits the tile's fixed work asks for 64; where both sizes are 64 or less, outputs take 32, with
+// which four blocks have room on a compute unit instead of two (gradient of 16 segments of 512 tokens, 8 heads of 64: 54 us with 64,
+// 46 with 32; 16384 tokens of 8 heads of 128: 73 and 87).  With 32 bits 64 would not fit, and 16 is hardly ever faster (16 segments
+// of 1000 tokens, 8 heads of 128: 235 us with 32, 271 with 16; 32 such segments, heads of 64: 146 and 142).
+constexpr int tile_positions(bool bf, int cols, int rows, bool main) { return bf && !(main && cols <= 64 && rows <= 64) ? 64 : 32; }
+
 template <class T, int CP, int RP, bool MAIN>
 struct ChunkLds {
     typedef Tile<T> W;
+    static constexpr int C = tile_positions(sizeof(T) == 2, CP, RP, MAIN);
     static constexpr int NT = CP > 64 || RP > 64 ? 512 : 256;                // threads: sixteen rows of the state per wavefront
-    static constexpr int COL = 0, ROW = COL + Image<T, CP>::BYTES, BY = ROW + Image<T, RP>::BYTES, SET = BY + (MAIN ? Image<T, CP>::BYTES : 0);
-    static constexpr int JB = W::C + W::VE;                                  // pitch of P
-    static constexpr int P = 2 * SET, PW = P + (MAIN ? W::C * JB * (int)sizeof(T) : 0), FW = PW + (W::C + 4) * 4, ODD = FW + W::C * 4, BYTES = ODD + 16;
+    static constexpr int COL = 0, ROW = COL + Image<T, C, CP>::BYTES, BY = ROW + Image<T, C, RP>::BYTES, SET = BY + (MAIN ? Image<T, C, CP>::BYTES : 0);
+    static constexpr int JB = C + W::VE;                                  // pitch of P
+    static constexpr int P = 2 * SET, PW = P + (MAIN ? C * JB * (int)sizeof(T) : 0), FW = PW + (C + 4) * 4, ODD = FW + C * 4, BYTES = ODD + 16;
 };
 
 // The lane's number as if it were new: places that are made of it are worked out where they are used, not kept in registers from
@@ -276,6 +283,11 @@ __device__ inline double power(double d, int e) {
         if (e & 1) r *= d;
     return r;
 }
+
+// The item that a block takes: eight neighbours change places, by one more in the next eight and in the next head.  Blocks go to the
+// eight dies in turn, and places without a span (one behind each segment that is whole spans long) would fall to some of them only
+// (gradient of 64 segments of 512 tokens in spans of 512, 8 heads of 64 and 128 bf16: 394 us without this, 265 with).
+__device__ inline int item_of(int i, int head) { return (i & ~7) | ((i + (i >> 3) + head) & 7); }
 
 // Which segment and which span of it the item is; false: none.  A wavefront looks at 64 places of the table at a time.
 // Where short segments are left to the other kernel there are no spans, and item i is the segment that token i * (brief + 1) lies
@@ -339,21 +351,21 @@ __device__ inline bool whole_pieces(const DecayView &v, int dim) {
 }
 // The tile of one tensor: n positions of the span, `lowest` the first of their tokens in memory, zeros behind them.
 // off: of this thread's piece in a whole tile (tile_offset).
-template <class T, int D, int NT>
+template <class T, int C, int D, int NT>
 __device__ inline uint32_t tile_offset(const DecayView &v, bool back, int tid) {
-    typedef Image<T, D> I;
+    typedef Image<T, C, D> I;
     const int pos = tid / I::PIECES, piece = tid % I::PIECES ^ I::order(pos);
-    return (uint32_t)(back ? Tile<T>::C - 1 - pos : pos) * (uint32_t)v.token * (uint32_t)sizeof(T) + piece * 16;
+    return (uint32_t)(back ? C - 1 - pos : pos) * (uint32_t)v.token * (uint32_t)sizeof(T) + piece * 16;
 }
-template <class T, int D, int NT>
+template <class T, int C, int D, int NT>
 __device__ inline void stage(const DecayView &v, int dim, bool whole, uint32_t off, int lowest, int n, bool back, int head, char *to, int wave) {
-    typedef Image<T, D> I;
+    typedef Image<T, C, D> I;
     constexpr int ALL = I::BYTES / 16, STEP = NT / I::PIECES;        // positions from one piece of a thread to the next
     static_assert(ALL % 64 == 0 && STEP % 16 == 0, "whole wavefronts, and a thread's rows in one order");
     const char *rows = (const char *)at<T>(v, lowest, head);
     const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + wave * 1024);
-    const bool full = whole && n == Tile<T>::C && dim == D;
+    const bool full = whole && n == C && dim == D;
 #pragma unroll
     for (int k = 0; k < (ALL + NT - 1) / NT; ++k) {
         if (ALL % NT && 64 * wave + NT * k >= ALL) break;
@@ -393,9 +405,9 @@ template <class T, int CP, int RP, bool MAIN, int TERMS>
 __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
     typedef Tile<T> W;
     typedef ChunkLds<T, CP, RP, MAIN> L;
-    typedef Image<T, CP> IC;
-    typedef Image<T, RP> IR;
-    constexpr int C = W::C, KB = W::KB, VE = W::VE, IT = C / 16, CT = CP / 16, KT = C / KB, NT = L::NT, WAVES = NT / 64;
+    typedef Image<T, L::C, CP> IC;
+    typedef Image<T, L::C, RP> IR;
+    constexpr int C = L::C, KB = W::KB, VE = W::VE, IT = C / 16, CT = CP / 16, KT = C / KB, NT = L::NT, WAVES = NT / 64;
     extern __shared__ uint4 lds4[];
     char *const lds = (char *)lds4;
     T *const P = (T *)(lds + L::P);
@@ -403,9 +415,9 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     int *const odd = (int *)(lds + L::ODD);
     const DecayPass &p = job.pass[blockIdx.z];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16, l16 = lane % 16;
-    const int item = blockIdx.x, head = blockIdx.y, heads = gridDim.y;
+    const int head = blockIdx.y, heads = gridDim.y, item = item_of(blockIdx.x, head);
     int seg, nth, first, end;
-    if (!find_item(job, item, seg, nth)) return;
+    if (item >= job.items || !find_item(job, item, seg, nth)) return;
     segment_tokens(job, seg, first, end);
     first = __builtin_amdgcn_readfirstlane(first); end = __builtin_amdgcn_readfirstlane(end);
     const int whole = end - first;
@@ -419,14 +431,14 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     const float d = job.decay[head];
     const bool fades = (float)power((double)d, C) == 0.f;           // some factors of a tile are zero
     const bool pieces = whole_pieces<T>(p.col, cols) && whole_pieces<T>(p.row, rows) && whole_pieces<T>(p.by, cols);
-    const uint32_t col_off = tile_offset<T, CP, NT>(p.col, back, tid), row_off = tile_offset<T, RP, NT>(p.row, back, tid),
-                   by_off = MAIN ? tile_offset<T, CP, NT>(p.by, back, tid) : 0;
+    const uint32_t col_off = tile_offset<T, C, CP, NT>(p.col, back, tid), row_off = tile_offset<T, C, RP, NT>(p.row, back, tid),
+                   by_off = MAIN ? tile_offset<T, C, CP, NT>(p.by, back, tid) : 0;
     int flag = 0;
     auto fetch = [&](int base, int n, char *set) {
         const int lowest = back ? end - base - n : first + base;
-        stage<T, CP, NT>(p.col, cols, pieces, col_off, lowest, n, back, head, set + L::COL, wave);
-        stage<T, RP, NT>(p.row, rows, pieces, row_off, lowest, n, back, head, set + L::ROW, wave);
-        if (MAIN) stage<T, CP, NT>(p.by, cols, pieces, by_off, lowest, n, back, head, set + L::BY, wave);
+        stage<T, C, CP, NT>(p.col, cols, pieces, col_off, lowest, n, back, head, set + L::COL, wave);
+        stage<T, C, RP, NT>(p.row, rows, pieces, row_off, lowest, n, back, head, set + L::ROW, wave);
+        if (MAIN) stage<T, C, CP, NT>(p.by, cols, pieces, by_off, lowest, n, back, head, set + L::BY, wave);
         if (job.starts) {
             // backward, the cut lies between a token and the one behind it
             const int pos = min(lane, n - 1), t = lowest + (back ? n - pos : pos);
@@ -843,7 +855,7 @@ hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipSt
         if (e != hipSuccess) return e;
         lds_set = lds;
     }
-    launch(kernel, dim3(job.items, heads, passes), dim3(ChunkLds<T, CP, RP, MAIN>::NT), lds, s, job);
+    launch(kernel, dim3((job.items + 7) / 8 * 8, heads, passes), dim3(ChunkLds<T, CP, RP, MAIN>::NT), lds, s, job);
     return hipGetLastError();
 }
 // States are fp32 where they are handed out: a bfloat16 key with its decay then goes in as three terms, else as one.
@@ -878,20 +890,27 @@ hipError_t by_sizes(const DecayJob &job, int passes, F go) {
     return hipSuccess;
 }
 
-// Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN.  Longer spans leave compute units
-// idle or wait for one another at the end, shorter ones begin more often (about three tiles' time) and leave more states behind.
-// Counted in tiles, with two blocks per compute unit if both sizes are above 64 and one if not.  Measured against twice and half of
-// what it picks, us of the kernels: 16384 tokens bf16, 8 heads of 128 (512): 84 / 93 and 101; 24 episodes of 6001 tokens fp32, 6 heads of
-// 48 and 80 (128): 59 / 94 with 256; gradient of 4096 tokens fp32, 4 heads of 128 (256): 98 / 112 with 128.
+// Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN, the one that takes least time by this
+// count.  A block's time is its tiles and three more for its beginning; blocks take turns on as many places as the compute units have.
+// If the longest segment (by guess, twice the average) is longer than the span there is the kernel before this one too, which takes
+// half of the time, and four tiles' time for what lies between the two.  Over 66 calls of 1 to 100 segments, equal and not,
+// of 4096 to 64000 tokens this is 3% behind the best of 128 to 1024 each time, 30% at most; us of all kernels with 128 / 256 / 512 /
+// 1024: 16384 tokens bf16, 8 heads of 128: 124 / 96 / 85 / 118 (512 taken); gradient of 4096 tokens fp32, 4 heads of 128:
+// 103 / 99 / 170 / 318 (256); gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (512).
 constexpr int SHORTEST_SPAN = 128;
 int span_of(int heads, int n_segments, int n_tokens, int key, int value, int passes, bool bf) {
-    const int tile = bf ? Tile<bf16>::C : Tile<float>::C;
-    const int64_t slots = key > 64 && value > 64 ? 256 : 512;
+    const bool small = key <= 64 && value <= 64;
+    const int tile = tile_positions(bf, key, value, true);
+    const int64_t slots = small && bf ? 1024 : key > 64 && value > 64 ? 256 : 512,
+                  longest = n_segments == 1 ? n_tokens : std::min<int64_t>(n_tokens, 2 * ((int64_t)n_tokens / n_segments));
     int best = 0;
     int64_t least = INT64_MAX;
     for (int span = SHORTEST_SPAN; span <= 1 << 20; span *= 2) {
-        const int64_t blocks = (n_tokens / span + n_segments / 2) * (int64_t)heads * passes;      // half of a segment's last span is not there
-        const int64_t time = std::max<int64_t>(1, (blocks + slots - 1) / slots) * (std::min(span, n_tokens) / tile + 3);
+        const bool split = span < longest;
+        auto rounds = [&](int64_t items) { return std::max<int64_t>(1, (items * heads + slots - 1) / slots); };
+        // half of a segment's last span is not there
+        int64_t time = 2 * rounds((split ? n_tokens / span + n_segments / 2 : n_segments) * (int64_t)passes) * (std::min<int64_t>(span, longest) / tile + 3);
+        if (split) time += rounds(std::max(1, n_tokens / span - n_segments / 2) * (int64_t)(passes > 1 ? 2 : 1)) * (span / tile + 3) + 8;
         if (time < least) { least = time; best = span; }
     }
     return best;
