@@ -459,7 +459,7 @@ typedef struct {
  *   S = 0 where starts[t] != 0;  S = decay S + v_t k_t^T;  out_t = scale S q_t
  * and state_out receives S behind the segment's last token.
  *   q, k          [n_tokens][n_heads][key_dim];  v, out [n_tokens][n_heads][value_dim]
- *                 (n_segments <= 2^24)
+ *                 (n_segments <= 2^22, n_tokens <= 2^28)
  *   seg_start_dev i32 [n_segments+1] as for ga3c_train_step_ragged (checked no
  *                 more than there: a bad table gives wrong results, no access
  *                 outside the arrays), or NULL: segments of equal length
@@ -471,7 +471,9 @@ typedef struct {
  *                 16-byte aligned, contents irrelevant before and after; calls
  *                 that may overlap need one each
  * Products of fp32 tensors and all states are fp32 sums; with bfloat16 tensors
- * an output is within a few roundings to bfloat16 of the exact one. */
+ * an output is within a few roundings to bfloat16 of the exact one.  A number
+ * that is not finite reaches what it is part of and nothing else; an infinity
+ * may arrive there as NaN. */
 int ga3c_decay_attention(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
                          const ga3c_heads *out, const int32_t *seg_start_dev, const uint8_t *starts_dev, int n_segments,
                          int n_tokens, const float *state_in_dev, float *state_out_dev, void *workspace_dev,
@@ -491,6 +493,7 @@ size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *desc, int n_segment
 
 /* One token of each of n agents, whose states lie in states_dev f32
  * [n_slots][n_heads][value_dim][key_dim] and are advanced in place.
+ *   n           at most 2^22
  *   slots_dev   i32 [n], the state of each token, or NULL: token i has state i
  *               (n <= n_slots then).  A slot outside [0, n_slots) is a padded
  *               entry: a state of zeros that is not kept.  Tokens that name the
@@ -508,8 +511,9 @@ int ga3c_decay_attention_step(const ga3c_decay_desc *desc, const ga3c_heads *q, 
  * with mean and (biased) variance over the sample's group, gamma and beta f32
  * [channels].  Position i of x starts at x + i * x_stride elements, i counting
  * through all samples; x_stride, y_stride >= channels.  At most 2^20 channels,
- * 2^24 samples and 2^24 positions; a sample far larger than a few GB may be
- * refused.
+ * 2^24 samples and 2^24 positions.  Refused as too large: a sample of more than
+ * 65535 times what a block holds (64 KB or more), and more samples than 2^32
+ * threads are enough for (at most 1024 for a sample's group).
  *   stats_dev   f32 [n_samples][groups][2] receives mean and rstd, which the
  *               gradient needs; may be NULL
  *   workspace_dev  as above, of ga3c_group_norm_workspace() bytes

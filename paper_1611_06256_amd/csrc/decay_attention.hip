@@ -896,7 +896,7 @@ hipError_t by_sizes(const DecayJob &job, int passes, F go) {
 // half of the time, and four tiles' time for what lies between the two.  Over 66 calls of 1 to 100 segments, equal and not,
 // of 4096 to 64000 tokens this is 3% behind the best of 128 to 1024 each time, 30% at most; us of all kernels with 128 / 256 / 512 /
 // 1024: 16384 tokens bf16, 8 heads of 128: 124 / 96 / 85 / 118 (512 taken); gradient of 4096 tokens fp32, 4 heads of 128:
-// 103 / 99 / 170 / 318 (256); gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (512).
+// 103 / 99 / 170 / 318 (256); gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (1024).
 constexpr int SHORTEST_SPAN = 128;
 int span_of(int heads, int n_segments, int n_tokens, int key, int value, int passes, bool bf) {
     const bool small = key <= 64 && value <= 64;
@@ -991,7 +991,8 @@ int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *
 }
 int check_segments(const int32_t *seg_start, int n_segments, int n_tokens, const char *who) {
     if (n_segments < 0 || n_tokens < 0) return call_fail(GA3C_EINVAL, "%s: negative count", who);
-    if (n_segments > 1 << 24) return call_fail(GA3C_EINVAL, "%s: more than 2^24 segments", who);
+    // threads of a launch are counted in 32 bits
+    if (n_segments > 1 << 22 || n_tokens > 1 << 28) return call_fail(GA3C_EINVAL, "%s: more than 2^22 segments or 2^28 tokens", who);
     if (n_segments == 0 && n_tokens > 0) return call_fail(GA3C_EINVAL, "%s: tokens without a segment", who);
     if (!seg_start && n_segments > 0 && n_tokens % n_segments) return call_fail(GA3C_EINVAL, "%s: %d tokens are no %d equal segments", who, n_tokens, n_segments);
     return GA3C_OK;
@@ -1099,6 +1100,7 @@ extern "C" int ga3c_decay_attention_step(const ga3c_decay_desc *d, const ga3c_he
     int rc = check_desc(d, who);
     if (rc != GA3C_OK) return rc;
     if (n < 0 || n_slots < 0) return call_fail(GA3C_EINVAL, "%s: negative count", who);
+    if (n > 1 << 22) return call_fail(GA3C_EINVAL, "%s: more than 2^22 tokens", who);
     if (n == 0) return GA3C_OK;
     if (!slots && n > n_slots) return call_fail(GA3C_EINVAL, "%s: %d tokens for %d states", who, n, n_slots);
     if (!states) return call_fail(GA3C_EINVAL, "%s: null states", who);

@@ -368,6 +368,26 @@ def test_group_norm_and_its_gradient(shape, act, dtype):
     norm_near(dbeta, want[2], 1.2 * (dz_tol + kk * dz.abs()).sum((0, 1)), "dbeta", F32)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 300001, 8, 2), (2, 70001, 24, 3), (3, 9000, 65, 5)], ids=["300001", "70001", "9000"])
+def test_group_norm_of_samples_of_many_chunks(shape, dtype):
+    test_group_norm_and_its_gradient(shape, "silu", dtype)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("shape", [(3, 1, 64, 4), (3, 20, 64, 4), (3, 5000, 64, 4), (2, 1, 4099, 1)], ids=["rows", "tiles", "chunks", "wide"])
+def test_group_norm_keeps_nan_to_its_group(shape, act):
+    n, p, c, groups = shape
+    x = torch.randn(n, p, c, generator=torch.Generator().manual_seed(1))
+    x[1, p // 2, 0] = float("nan")
+    y, w = torch.empty(n, p, c, device="cuda"), torch.ones(c, device="cuda")
+    g.group_norm(x.cuda(), w, 0 * w, groups, y, act=act)
+    torch.cuda.synchronize()
+    want = torch.zeros(n, p, c, dtype=torch.bool)
+    want[1, :, :c // groups] = True
+    assert torch.equal(torch.isnan(y).cpu(), want)
+
+
 def test_group_norm_of_no_samples_and_of_a_constant():
     z = torch.empty(0, 5, 32, device="cuda")
     w, b = torch.ones(32, device="cuda"), torch.zeros(32, device="cuda")

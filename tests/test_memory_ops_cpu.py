@@ -128,6 +128,21 @@ def test_group_norm_refuses():
         assert grad(**kw) == -1, kw
 
 
+def test_calls_that_are_too_large_are_refused():
+    lib = g.load_library()
+    d, v = desc(), views(8, [16, 16, 32, 32])
+    assert forward(lib, d, v, n_segments=(1 << 22) + 1, n_tokens=1 << 24, table=A) == -1 and b"2^22 segments" in lib.ga3c_last_error()
+    assert forward(lib, d, v, n_segments=1, n_tokens=(1 << 28) + 1) == -1 and b"2^28 tokens" in lib.ga3c_last_error()
+    n = (1 << 22) + 1
+    assert lib.ga3c_decay_attention_step(C.byref(d), *[C.byref(x) for x in v], None, None, n, A, n, None) == -1
+    assert b"2^22 tokens" in lib.ga3c_last_error()
+    # one position (rows), a few, and groups wider than a block
+    for channels, groups, samples, positions in ((1024, 256, 1 << 24, 1), (64, 4, 1 << 24, 4), (1 << 20, 128, 1 << 24, 1)):
+        nd = binding._NormDesc(channels, groups, 1, 0, 1e-5)
+        rc = lib.ga3c_group_norm(C.byref(nd), A, channels, A, A, A + (1 << 30), channels, None, samples, positions, A, 1 << 60, None)
+        assert rc == -1 and b"too many samples" in lib.ga3c_last_error(), channels
+
+
 def test_binding_refuses_cpu_tensors():
     x = torch.zeros(4, 2, 16)
     with pytest.raises(g.Ga3cError, match="GPU tensor"):
