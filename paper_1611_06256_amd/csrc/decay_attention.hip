@@ -975,12 +975,12 @@ int check_views(const ga3c_heads *const *in, int n_in, const ga3c_heads *const *
         if (!in[i] || !in[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)in[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
         if (in[i]->token_stride < 0 || in[i]->head_stride < 0) return call_fail(GA3C_EINVAL, "%s: negative stride", who);
-        if (in[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
+        if (n > 1 && in[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
     }
     for (int i = 0; i < n_out; ++i) {
         if (!out[i] || !out[i]->data) return call_fail(GA3C_EINVAL, "%s: null tensor", who);
         if ((uintptr_t)out[i]->data % size) return call_fail(GA3C_EINVAL, "%s: tensor not aligned to its elements", who);
-        if (out[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
+        if (n > 1 && out[i]->token_stride >= MAX_STRIDE) return call_fail(GA3C_EINVAL, "%s: token_stride of 2^24 or more", who);
         if (!apart(*out[i], n, heads, out_dims[i])) return call_fail(GA3C_EINVAL, "%s: strides make rows of an output overlap", who);
         for (int k = 0; k < n_in; ++k)
             if (out[i]->data == in[k]->data) return call_fail(GA3C_EINVAL, "%s: an output is one of the inputs", who);

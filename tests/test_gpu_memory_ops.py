@@ -211,6 +211,79 @@ def test_a_bad_table_stays_within_the_arrays():
 # ------------------------------------------------------------------- single tokens --
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[4, 1, 0, 9], [300, 700, 0, 65]], ids=["short", "long"])
+def test_rows_outside_the_segments_are_left_as_they_were(lens, dtype):
+    front, rear, h, dk, dv, decay = 7, 140, 3, 32, 48, [0.5, 0.95, 0.99]
+    s = make([front] + lens + [rear], h, dk, dv, dtype, False, 0.02, False)
+    n, end = front + sum(lens) + rear, front + sum(lens)
+    inside = torch.tensor([front], dtype=torch.int32, device="cuda") + torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32).cuda()
+    for k in ("q", "k", "v", "dout"):         # what lies there is nobody's
+        s[k][:front] = float("nan")
+        s[k][end:] = float("inf")
+    e = lambda d: torch.full((n, h, d), 7.0, dtype=dtype, device="cuda")  # noqa: E731
+    got = [e(dv), e(dk), e(dk), e(dv)]
+    g.decay_attention(s["q"], s["k"], s["v"], decay, got[0], seg_start=inside, starts=s["starts"])
+    g.decay_attention_grad(s["q"], s["k"], s["v"], decay, s["dout"], *got[1:], seg_start=inside, starts=s["starts"])
+    part = {k: s[k][front:end].contiguous() for k in ("q", "k", "v", "dout", "starts")}
+    want = [t[front:end].clone() for t in (e(dv), e(dk), e(dk), e(dv))]
+    g.decay_attention(part["q"], part["k"], part["v"], decay, want[0], seg_start=inside - front, starts=part["starts"])
+    g.decay_attention_grad(part["q"], part["k"], part["v"], decay, part["dout"], *want[1:], seg_start=inside - front, starts=part["starts"])
+    torch.cuda.synchronize()
+    args = [wide(part[x]) for x in ("q", "k", "v", "dout")]
+    factors = 2 * max(lens) + max(dk, dv) + 24
+    exact, size = [], []
+    for x, to in ((args, exact), ([t.abs() for t in args], size)):
+        to.append(ref.attention(*x[:3], decay, lens, wide(part["starts"]))[0])
+        to += ref.attention_grad(*x[:3], decay, lens, x[3], wide(part["starts"]))[:3]
+    for what, a, b, x, m in zip(("out", "dq", "dk", "dv"), got, want, exact, size):
+        assert bool((a[:front] == 7).all()) and bool((a[end:] == 7).all()), what
+        near(a[front:end], x, m, factors, what, dtype)
+        near(b, x, m, factors, what, dtype)
+
+
+def test_two_calls_at_once_on_two_streams():
+    lens, h, dk, dv, decay = [3000, 900, 5000], 4, 64, 64, [0.9, 0.97, 0.99, 0.999]
+    sets = [make(lens, h, dk, dv, F32, True, 0.001, False, seed=i) for i in range(2)]
+    n = sum(lens)
+
+    def run(s, stream=None):
+        e = lambda d: torch.empty(n, h, d, device="cuda")  # noqa: E731
+        out = [e(dv), e(dk), e(dk), e(dv), torch.empty_like(s["state_in"]), torch.empty_like(s["state_in"])]
+        torch.cuda.synchronize()
+        seg = dict(seg_start=s["seg_start"], starts=s["starts"], state_in=s["state_in"], stream=stream)
+
+        def go():
+            g.decay_attention(s["q"], s["k"], s["v"], decay, out[0], state_out=out[4], **seg)
+            g.decay_attention_grad(s["q"], s["k"], s["v"], decay, s["dout"], *out[1:4], dstate_out=s["dstate_out"], dstate_in=out[5], **seg)
+        return go, out
+    alone = [run(s) for s in sets]
+    for go, _ in alone:
+        go()
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    both = [run(s, stream) for s, stream in zip(sets, streams)]
+    for _ in range(4):
+        for go, _ in both:
+            go()
+    torch.cuda.synchronize()
+    for (_, a), (_, b) in zip(alone, both):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_single_token_of_a_wide_matrix():
+    """One token's distance to the next is nobody's business."""
+    h, dk, dv = 2, 8, 8
+    m = torch.randn(1, h * (2 * dk + dv), generator=torch.Generator().manual_seed(5)).cuda()
+    q, k, v = (t.unflatten(1, (h, 8)).as_strided((1, h, 8), (1 << 30, 8, 1)) for t in (m[:, :16], m[:, 16:32], m[:, 32:]))
+    out, state = torch.empty(1, h, dv, device="cuda"), torch.empty(1, h, dv, dk, device="cuda")
+    g.decay_attention(q, k, v, [0.5, 0.9], out, state_out=state)
+    torch.cuda.synchronize()
+    want = wide(v)[0][:, :, None] * wide(k)[0][:, None, :]
+    assert float((wide(state)[0] - want).abs().max()) <= 1e-6 * float(want.abs().max())
+    assert float((wide(out)[0] - (want @ wide(q)[0][:, :, None])[..., 0]).abs().max()) <= 1e-5 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("n,slots,h,dk,dv", [(1, 1, 1, 1, 1), (1, 5, 4, 16, 32), (7, 20, 2, 17, 33), (33, 64, 3, 64, 64), (64, 64, 2, 128, 128),
                                              (300, 400, 2, 48, 80)])
 def test_steps(n, slots, h, dk, dv, dtype):
