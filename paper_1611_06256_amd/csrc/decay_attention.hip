@@ -34,6 +34,16 @@ __device__ inline const T *at(const DecayView &v, int token, int head) { return 
 // A wavefront takes RPL * 64 / LPR rows of one segment's state in one head: LPR lanes share a row, four columns each (or twice
 // four), and a lane has RPL rows.  Bound by the latency of memory: the tokens come eight (or four) at a time, so that those of a
 // segment of an update are on their way together.
+// Sum over LPR neighbouring lanes, the same in all of them: lanes trade within fours, then eight and sixteen mirrored, without LDS.
+template <int HOW>
+__device__ inline float traded(float v) { return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), HOW, 0xf, 0xf, true)); }
+template <int LPR>
+__device__ inline float row_sum(float v) {
+    v = traded<0x4e>(traded<0xb1>(v));        // lane ^ 1, lane ^ 2
+    if (LPR >= 8) v = traded<0x141>(v);       // 7 - lane of eight
+    if (LPR >= 16) v = traded<0x140>(v);      // 15 - lane of sixteen
+    return v;
+}
 template <int RPL, int CV>
 struct Rows {
     float4 x[RPL][CV];
@@ -51,8 +61,7 @@ struct Rows {
                 y.z = keep * y.z + row[i] * col[v].z; y.w = keep * y.w + row[i] * col[v].w;
                 sum[i] += y.x * by[v].x + y.y * by[v].y + y.z * by[v].z + y.w * by[v].w;
             }
-#pragma unroll
-            for (int m = LPR / 2; m > 0; m /= 2) sum[i] += __shfl_xor(sum[i], m);
+            sum[i] = row_sum<LPR>(sum[i]);
         }
     }
     __device__ void fade(float f) {
@@ -289,6 +298,9 @@ __device__ inline double power(double d, int e) {
 // (gradient of 64 segments of 512 tokens in spans of 512, 8 heads of 64 and 128 bf16: 394 us without this, 265 with).
 __device__ inline int item_of(int i, int head) { return (i & ~7) | ((i + (i >> 3) + head) & 7); }
 
+// (The state that span k of a segment makes of nothing, if it is not its last one, has place first token / span + k.  That is less than
+// the place of the next segment's first: scratch is n_tokens / span places, however many segments there are.)
+//
 // Which segment and which span of it the item is; false: none.  A wavefront looks at 64 places of the table at a time.
 // Where short segments are left to the other kernel there are no spans, and item i is the segment that token i * (brief + 1) lies
 // in, if no smaller one does: a segment that is longer than `brief` holds one of these.
@@ -334,12 +346,19 @@ __device__ inline void piece_to_lds(const void *from, uint32_t lds) {
 __device__ inline void piece_to_lds(const void *base, uint32_t off, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
-// VE elements of a row from element `i` on, zero behind its `dim` elements; rows begin anywhere.
+// VE elements of a row from element `i` on, zero behind its `dim` elements; rows begin anywhere.  pairs: at four bytes or their
+// multiples, and end there.
 template <class T>
-__device__ inline uint4 loose_piece(const T *row, int i, int dim) {
+__device__ inline uint4 loose_piece(const T *row, int i, int dim, bool pairs) {
     constexpr int VE = Tile<T>::VE;
-    union { uint4 u; T e[VE]; } r;
+    union { uint4 u; uint32_t w[4]; T e[VE]; } r;
     r.u = uint4{0, 0, 0, 0};
+    if (sizeof(T) == 2 && pairs) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + 2 * k < dim) r.w[k] = *(const uint32_t *)(row + i + 2 * k);
+        return r.u;
+    }
 #pragma unroll
     for (int k = 0; k < VE; ++k)
         if (i + k < dim) r.e[k] = row[i + k];
@@ -365,7 +384,7 @@ __device__ inline void stage(const DecayView &v, int dim, bool whole, uint32_t o
     const char *rows = (const char *)at<T>(v, lowest, head);
     const uint32_t step = (uint32_t)v.token * (uint32_t)sizeof(T);
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + wave * 1024);
-    const bool full = whole && n == C && dim == D;
+    const bool full = whole && n == C && dim == D, pairs = (uintptr_t)v.data % 4 == 0 && ((v.token | v.head | dim) % 2) == 0;
 #pragma unroll
     for (int k = 0; k < (ALL + NT - 1) / NT; ++k) {
         if (ALL % NT && 64 * wave + NT * k >= ALL) break;
@@ -380,7 +399,7 @@ __device__ inline void stage(const DecayView &v, int dim, bool whole, uint32_t o
             piece_to_lds(pos < n && i < dim ? (const void *)(row + piece * 16) : (const void *)decay_nothing, lds + NT * 16 * k);
         else {
             uint4 u{0, 0, 0, 0};
-            if (pos < n && i < dim) u = loose_piece((const T *)row, i, dim);
+            if (pos < n && i < dim) u = loose_piece((const T *)row, i, dim, pairs);
             *(uint4 *)(to + s * 16) = u;
         }
     }
@@ -453,7 +472,8 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     // the state: tile ct holds X[r][.] of row r = 16 wave + l16 and the four columns from 16 ct + 4 g on
     const size_t size = (size_t)rows * cols;
     const int row_step = turned ? 1 : cols, col_step = turned ? rows : 1;
-    const float *x_in = nth > 0 && MAIN ? p.spans + ((size_t)(item - 1) * heads + head) * size
+    const size_t place = (size_t)(first / job.span + nth) * heads + head;      // of the span's state
+    const float *x_in = nth > 0 && MAIN ? p.spans + (place - heads) * size
                                         : MAIN && p.x_in ? p.x_in + ((size_t)seg * heads + head) * size : nullptr;
     f32x4 x[CT];
     const int r = 16 * wave + l16;
@@ -632,8 +652,8 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
         }
         set = L::SET - set;
     }
-    float *x_out = !MAIN ? p.spans + ((size_t)item * heads + head) * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
-    if (!MAIN && tid == 0) p.spans[(size_t)job.items * heads * size + (size_t)item * heads + head] = passes ? 1.f : 0.f;
+    float *x_out = !MAIN ? p.spans + place * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
+    if (!MAIN && tid == 0) p.spans[(size_t)(job.n_tokens / job.span) * heads * size + place] = passes ? 1.f : 0.f;
     if (!x_out || !mine) return;
     const bool quads_out = !turned && cols % 4 == 0 && (uintptr_t)x_out % 16 == 0;
     const bool nothing = MAIN && back && whole > 0 && job.starts && job.starts[first];      // the first token knows of no state
@@ -663,9 +683,9 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
     const int e = ((blockIdx.z % parts) * 256 + threadIdx.x) * (QUAD ? 4 : 1);
     const size_t size = (size_t)p.rows * p.cols;
     if (e >= (int)size) return;
-    const int item = job.seg_start ? first / job.span + seg : seg * (job.len / job.span + 1);
-    float *at_span = p.spans + ((size_t)item * heads + head) * size + e;
-    const float *passes = p.spans + (size_t)job.items * heads * size + (size_t)item * heads + head;
+    const size_t place = (size_t)(first / job.span) * heads + head;
+    float *at_span = p.spans + place * size + e;
+    const float *passes = p.spans + (size_t)(job.n_tokens / job.span) * heads * size + place;
     const float w = (float)power((double)job.decay[head], job.span);
     V x{};
     if (p.x_in) __builtin_memcpy(&x, p.x_in + ((size_t)seg * heads + head) * size + e, sizeof x);
@@ -833,12 +853,14 @@ hipError_t by_shape(int rows, int cols, F go) {
 // States of a call from which on they pass the caches by.
 constexpr size_t STREAM_BYTES = (size_t)64 << 20;
 
-// Token by token: the passes of the job, all with rows and columns of the same sizes.
+// Token by token: the passes of the job.
 template <class T>
 hipError_t launch_recurrent(const DecayJob &job, int passes, int heads, hipStream_t s) {
-    return by_shape(job.pass[0].rows, job.pass[0].cols, [&](auto lpr, auto cv, auto rpl) {
+    int rows = 0, cols = 0;
+    for (int i = 0; i < passes; ++i) { rows = std::max(rows, job.pass[i].rows); cols = std::max(cols, job.pass[i].cols); }
+    return by_shape(rows, cols, [&](auto lpr, auto cv, auto rpl) {
         constexpr int ROWS = 64 / lpr.value * rpl.value;
-        const int slabs = (job.pass[0].rows + ROWS - 1) / ROWS;
+        const int slabs = (rows + ROWS - 1) / ROWS;
         const int64_t units = (int64_t)job.n_segments * slabs;
         launch(decay_recurrent_kernel<T, lpr.value, cv.value, rpl.value>, dim3((unsigned)((units + 3) / 4), heads, passes), dim3(256), 0, s, job, slabs);
         return hipGetLastError();
@@ -874,21 +896,28 @@ hipError_t launch_chunk(const DecayJob &job, int passes, int heads, hipStream_t 
     return wide_rows ? launch_chunk_terms<T, 64, 128, MAIN>(job, passes, heads, s) : launch_chunk_terms<T, 64, 64, MAIN>(job, passes, heads, s);
 }
 
-// Calls go(job, passes) for each group of passes with the same sizes of rows and columns.
-template <class F>
-hipError_t by_sizes(const DecayJob &job, int passes, F go) {
+// Calls go(job, passes) for each group of passes that one launch can take: those that `together` says of.
+template <class Together, class F>
+hipError_t by_sizes(const DecayJob &job, int passes, Together together, F go) {
     bool done[3] = {false, false, false};
     for (int i = 0; i < passes; ++i) {
         if (done[i]) continue;
         DecayJob some = job;
         int n = 0;
         for (int k = i; k < passes; ++k)
-            if (!done[k] && job.pass[k].rows == job.pass[i].rows && job.pass[k].cols == job.pass[i].cols) { some.pass[n++] = job.pass[k]; done[k] = true; }
+            if (!done[k] && together(job.pass[i], job.pass[k])) { some.pass[n++] = job.pass[k]; done[k] = true; }
         const hipError_t e = go(some, n);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
+// Token by token: passes of small states share a launch, with room for the larger sizes (gradient of 32 segments of 5 tokens, 4 heads
+// of 16 and 32: 22 us apart, 16 together; of 512 such segments 29 and 25, with heads of 32 and 64 56 and 96).
+bool recurrent_together(const DecayPass &a, const DecayPass &b) {
+    return (a.rows == b.rows && a.cols == b.cols) || std::max({a.rows, a.cols, b.rows, b.cols}) <= 32;
+}
+// Chunked: passes of one kernel (gradient of 64 segments of 256 tokens bf16, 4 heads of 64 and 32: 58 us apart, 37 together).
+bool chunk_together(const DecayPass &a, const DecayPass &b) { return (a.rows > 64) == (b.rows > 64) && (a.cols > 64) == (b.cols > 64); }
 
 // Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN, the one that takes least time by this
 // count.  A block's time is its tiles and three more for its beginning; blocks take turns on as many places as the compute units have.
@@ -915,19 +944,27 @@ int span_of(int heads, int n_segments, int n_tokens, int key, int value, int pas
     }
     return best;
 }
-// Segments of up to so many tokens take the token-by-token kernel if the average is short.
-constexpr int BRIEF = 32;
+// The average length up to which segments take the token-by-token kernel (those of up to twice that, the rest are chunked).  What that
+// kernel does for a token grows with the state, the chunked one has its fixed work per segment, which takes longer with 32 bits.  us
+// token by token / chunked, 128 and 768 segments of 4 heads: fp32 16 and 32, 15 tokens 20 / 22 and 28 / 60; 32 and 32, 10 tokens
+// 21 / 23 and 28 / 58; 64 and 64, 7 tokens 19 / 22 and 54 / 62, 10 tokens 24 / 22 and 73 / 63; bf16 16 and 16, 10 tokens 18 / 20 and
+// 21 / 30; 32 and 32, 4.5 tokens 19 / 19 and 22 / 31, 10 tokens 29 / 20 and 34 / 31; 64 and 64, 2 tokens 12 / 20 and 35 / 33, 4.5
+// tokens 20 / 20 and 51 / 34.
+int brief_average(int key, int value, bool bf) {
+    const int size = key * value;
+    if (bf) return size <= 256 ? 12 : size <= 1024 ? 5 : 3;
+    return size <= 512 ? 16 : size <= 1024 ? 10 : 7;
+}
 
 void plan(DecayJob &job, const ga3c_decay_desc *d, bool grad) {
-    job.brief = job.n_tokens / job.n_segments <= BRIEF / 2 ? BRIEF : -1;
-    job.span = job.brief >= 0 ? 1 << 30 : span_of(d->n_heads, job.n_segments, job.n_tokens, d->key_dim, d->value_dim, grad ? 3 : 1, d->dtype == GA3C_BF16);
+    const bool bf = d->dtype == GA3C_BF16;
+    const int average = brief_average(d->key_dim, d->value_dim, bf);
+    job.brief = job.n_tokens <= average * (int64_t)job.n_segments ? 2 * average : -1;
+    job.span = job.brief >= 0 ? 1 << 30 : span_of(d->n_heads, job.n_segments, job.n_tokens, d->key_dim, d->value_dim, grad ? 3 : 1, bf);
     job.items = job.brief >= 0 ? job.n_tokens / (job.brief + 1) + 1
                                : job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
 }
-size_t spans_floats(const DecayJob &job, int heads, size_t size) {
-    const int longest = job.seg_start ? job.n_tokens : job.len;
-    return longest <= job.span ? 0 : (size_t)job.items * heads * (size + 1);
-}
+size_t spans_floats(const DecayJob &job, int heads, size_t size) { return (size_t)(job.n_tokens / job.span) * heads * (size + 1); }
 
 // passes: of outputs; sources: those of them whose spans' states are made (one forward, one backward)
 template <class T>
@@ -935,12 +972,12 @@ hipError_t run_job(DecayJob &job, int passes, const int *sources, int n_sources,
     const int longest = job.seg_start ? job.n_tokens : job.len;
     hipError_t e = hipSuccess;
     if (job.brief >= 0 && (job.seg_start || longest <= job.brief))
-        e = by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_recurrent<T>(some, n, heads, s); });
+        e = by_sizes(job, passes, recurrent_together, [&](const DecayJob &some, int n) { return launch_recurrent<T>(some, n, heads, s); });
     if (e != hipSuccess || longest <= job.brief) return e;
     if (longest > job.span) {
         DecayJob made = job;
         for (int i = 0; i < n_sources; ++i) made.pass[i] = job.pass[sources[i]];
-        e = by_sizes(made, n_sources, [&](const DecayJob &some, int n) { return launch_chunk<T, false>(some, n, heads, s); });
+        e = by_sizes(made, n_sources, chunk_together, [&](const DecayJob &some, int n) { return launch_chunk<T, false>(some, n, heads, s); });
         if (e != hipSuccess) return e;
         // four numbers per thread where that leaves enough blocks (one segment of 16384 tokens: 10 us, with four 16)
         const int size = job.pass[0].rows * job.pass[0].cols;
@@ -949,7 +986,7 @@ hipError_t run_job(DecayJob &job, int passes, const int *sources, int n_sources,
         launch(quad ? decay_spans_kernel<true> : decay_spans_kernel<false>, dim3(job.n_segments, heads, parts * n_sources), dim3(256), 0, s, made, parts);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    return by_sizes(job, passes, [&](const DecayJob &some, int n) { return launch_chunk<T, true>(some, n, heads, s); });
+    return by_sizes(job, passes, chunk_together, [&](const DecayJob &some, int n) { return launch_chunk<T, true>(some, n, heads, s); });
 }
 
 int check_desc(const ga3c_decay_desc *d, const char *who) {
@@ -1027,16 +1064,13 @@ using namespace ga3c;
 
 extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n_segments, int n_tokens, int grad) {
     if (check_desc(d, "ga3c_decay_attention_workspace") != GA3C_OK || n_segments < 1 || n_tokens < 1) return 0;
-    // as with a table, which needs the most; the gradient has states of both directions
+    // the gradient has states of both directions
     const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens, grad);
     return (grad ? 2 : 1) * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
 }
 
 size_t ga3c::decay_workspace_most(const ga3c_decay_desc *d, int n_tokens) {
-    if (n_tokens <= SHORTEST_SPAN) return 0;
-    // segments that are not brief, and places for spans in between
-    const size_t items = (size_t)n_tokens / (BRIEF / 2 + 1) + 1 + n_tokens / SHORTEST_SPAN;
-    return 2 * sizeof(float) * items * d->n_heads * ((size_t)d->key_dim * d->value_dim + 1);
+    return 2 * sizeof(float) * (n_tokens / SHORTEST_SPAN) * d->n_heads * ((size_t)d->key_dim * d->value_dim + 1);
 }
 
 extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,

@@ -29,7 +29,7 @@ struct DecayJob {
     const uint8_t *starts;           // nullptr: none
     int n_segments, n_tokens, len;
     int span;                        // tokens of a segment that one block of the chunked kernels takes
-    int items;                       // places for spans: those of segment i begin at seg_start[i] / span + i
+    int items;                       // blocks' places for spans: those of segment i begin at seg_start[i] / span + i
     int brief;                       // segments of up to so many tokens go to the token-by-token kernel, longer ones to the chunked,
                                      // in one span each; -1: all to the chunked
     float decay[GA3C_MAX_HEADS];
