@@ -921,11 +921,12 @@ bool chunk_together(const DecayPass &a, const DecayPass &b) { return (a.rows > 6
 
 // Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN, the one that takes least time by this
 // count.  A block's time is its tiles and three more for its beginning; blocks take turns on as many places as the compute units have.
-// If the longest segment (by guess, twice the average) is longer than the span there is the kernel before this one too, which takes
-// half of the time, and four tiles' time for what lies between the two.  Over 66 calls of 1 to 100 segments, equal and not,
-// of 4096 to 64000 tokens this is 3% behind the best of 128 to 1024 each time, 30% at most; us of all kernels with 128 / 256 / 512 /
-// 1024: 16384 tokens bf16, 8 heads of 128: 124 / 96 / 85 / 118 (512 taken); gradient of 4096 tokens fp32, 4 heads of 128:
-// 103 / 99 / 170 / 318 (256); gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (1024).
+// Two more kernels, two tiles' time, are launched unless no segment can be longer than the span; if the longest segment (by guess,
+// twice the average) is longer, they take half of the time of the outputs and as long again for what lies between.  Over 250 calls of
+// 1 to 100 segments, equal, uneven and cut at random, of 200 to 64000 tokens this is 7% behind the best of 128 to 1024 each time, 77%
+// at most (random cuts, whose longest segment is longer than guessed); us of all kernels with 128 / 256 / 512 / 1024: 16384 tokens
+// bf16, 8 heads of 128: 124 / 96 / 85 / 118 (512 taken); gradient of 4096 tokens fp32, 4 heads of 128: 103 / 99 / 170 / 318 (256);
+// gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (1024).
 constexpr int SHORTEST_SPAN = 128;
 int span_of(int heads, int n_segments, int n_tokens, int key, int value, int passes, bool bf) {
     const bool small = key <= 64 && value <= 64;
@@ -939,7 +940,8 @@ int span_of(int heads, int n_segments, int n_tokens, int key, int value, int pas
         auto rounds = [&](int64_t items) { return std::max<int64_t>(1, (items * heads + slots - 1) / slots); };
         // half of a segment's last span is not there
         int64_t time = 2 * rounds((split ? n_tokens / span + n_segments / 2 : n_segments) * (int64_t)passes) * (std::min<int64_t>(span, longest) / tile + 3);
-        if (split) time += rounds(std::max(1, n_tokens / span - n_segments / 2) * (int64_t)(passes > 1 ? 2 : 1)) * (span / tile + 3) + 8;
+        if (n_tokens > span) time += 4;
+        if (split) time += rounds(std::max(1, n_tokens / span - n_segments / 2) * (int64_t)(passes > 1 ? 2 : 1)) * (span / tile + 3) + 4;
         if (time < least) { least = time; best = span; }
     }
     return best;
