@@ -512,7 +512,7 @@ int ga3c_decay_attention_step(const ga3c_decay_desc *desc, const ga3c_heads *q, 
  * [channels].  Position i of x starts at x + i * x_stride elements, i counting
  * through all samples; x_stride, y_stride >= channels.  At most 2^20 channels,
  * 2^24 samples and 2^24 positions.  Refused as too large: a sample of more than
- * 65535 times what a block holds (64 KB or more), and more samples than 2^32
+ * 65535 times what a block holds (32 KB or more), and more samples than 2^32
  * threads are enough for (at most 1024 for a sample's group).
  *   stats_dev   f32 [n_samples][groups][2] receives mean and rstd, which the
  *               gradient needs; may be NULL

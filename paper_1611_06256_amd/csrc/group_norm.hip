@@ -60,7 +60,7 @@ __device__ inline float activation_slope(float z) {
     return 1.f;
 }
 
-// VE neighbouring elements as they lie in memory: 16 bytes, or a single one.  again(): what was made of them so far is not kept in
+// VE neighbouring elements as they lie in memory: 16 bytes, two, or a single one.  again(): what was made of them so far is not kept in
 // registers for what comes, but made anew.
 template <class T, int VE> struct Pack;
 template <> struct Pack<float, 4> {
@@ -83,6 +83,18 @@ template <> struct Pack<bf16, 8> {
     __device__ static Pack of(const float (&f)[8]) { return Pack{uint4{two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7])}}; }
     __device__ void again() { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 };
+template <> struct Pack<float, 2> {
+    float2 v;
+    __device__ float operator[](int i) const { return i == 0 ? v.x : v.y; }
+    __device__ static Pack of(const float (&f)[2]) { return Pack{float2{f[0], f[1]}}; }
+    __device__ void again() { asm volatile("" : "+v"(v.x), "+v"(v.y)); }
+};
+template <> struct Pack<bf16, 2> {
+    uint32_t v;
+    __device__ float operator[](int i) const { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
+    __device__ static Pack of(const float (&f)[2]) { return Pack{Pack<bf16, 8>::two(f[0], f[1])}; }
+    __device__ void again() { asm volatile("" : "+v"(v)); }
+};
 template <class T> struct Pack<T, 1> {
     T v;
     __device__ float operator[](int) const { return to_f32(v); }
@@ -91,7 +103,9 @@ template <class T> struct Pack<T, 1> {
 };
 template <int VE>
 __device__ inline void weights(float (&w)[VE], const float *p) {
-    if constexpr (VE == 1) w[0] = p[0];
+    if constexpr (VE < 4)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) w[i] = p[i];
     else
 #pragma unroll
         for (int i = 0; i < VE; i += 4) {
@@ -292,8 +306,10 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const NormArgs a) {
     if (lane == 0) *(float2 *)s = float2{first, second};
 }
 
+// Eight wavefronts per SIMD, so that two blocks of 1024 threads share a compute unit and one reads while the other writes (64 maps of
+// 1024 positions, 512 channels bf16: 39 us with one, 31 with two: 4.3 TB/s).
 template <class T, int VE, int NT, int NV, int MODE, int ACT>
-__global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
+__global__ __launch_bounds__(NT, 8) void norm_tile_kernel(const NormArgs a) {
     typedef Pack<T, VE> V;
     __shared__ float each[NT], mean_of[MAX_TILE_GROUPS], rstd_of[MAX_TILE_GROUPS];
     const int sample = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, first = MODE == TILE ? 0 : blockIdx.y * a.chunk;
@@ -305,7 +321,10 @@ __global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
     const T *x = (const T *)a.x + start * a.xs + channel;
     V in[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) in[j] = *(const V *)(x + min(w.row + w.rows * j, positions - 1) * a.xs);
+    for (int j = 0; j < NV; ++j) {
+        if (w.rows * j >= positions) continue;               // the same in all threads: nothing is done for positions that are not there
+        in[j] = *(const V *)(x + (w.row + w.rows * j < positions ? (w.row + w.rows * j) * a.xs : 0));
+    }
     if constexpr (MODE == CHUNK_RESULT) {
         for (int g = threadIdx.x; g < groups; g += NT) {
             const float2 st = *(const float2 *)(a.sums + 2 * ((int64_t)sample * a.chunks * a.groups + g0 + g));
@@ -316,23 +335,26 @@ __global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
         const float m = (float)positions * (float)a.wide;
         float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+            if (w.rows * j >= positions) continue;
             if (w.c >= 0 && w.row + w.rows * j < positions)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) s += in[j][e];
+        }
         group_sums<NT>(a, w, groups, s, each, mean_of);
         const float mean = mean_of[w.group] / m;
         s = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) in[j].again();
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+            if (w.rows * j >= positions) continue;
+            in[j].again();
             if (w.c >= 0 && w.row + w.rows * j < positions)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
                     const float d = in[j][e] - mean;
                     s += d * d;
                 }
+        }
         group_sums<NT>(a, w, groups, s, each, rstd_of);
         if constexpr (MODE == CHUNK_SUMS) {
             for (int g = threadIdx.x; g < groups; g += NT)
@@ -346,19 +368,25 @@ __global__ __launch_bounds__(NT) void norm_tile_kernel(const NormArgs a) {
         for (int g = threadIdx.x; g < groups; g += NT) *(float2 *)(a.stats + 2 * ((int64_t)sample * a.groups + g0 + g)) = float2{mean_of[g], rstd_of[g]};
     if (w.c < 0) return;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) in[j].again();
+    for (int j = 0; j < NV; ++j) {
+        if (w.rows * j >= positions) continue;
+        in[j].again();
+    }
     const float mean = mean_of[w.group], rstd = rstd_of[w.group];
     float g[VE], b[VE];
     weights<VE>(g, a.gamma + channel);
     weights<VE>(b, a.beta + channel);
     T *y = (T *)a.y + start * a.ys + channel;
+    int row = w.row;
+    asm volatile("" : "+v"(row));                    // places are worked out anew: they are too many to keep
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if (w.row + w.rows * j >= positions) break;
+        if (row + w.rows * j >= positions) break;
+        __builtin_amdgcn_sched_barrier(0);
         float z[VE];
 #pragma unroll
         for (int e = 0; e < VE; ++e) z[e] = activation<ACT>((in[j][e] - mean) * rstd * g[e] + b[e]);
-        *(V *)(y + (w.row + w.rows * j) * a.ys) = V::of(z);
+        *(V *)(y + (row + w.rows * j) * a.ys) = V::of(z);
     }
 }
 
@@ -386,6 +414,7 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
         asm volatile("" : "+v"(row));                // places are worked out in each round: they are too many to keep
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (w.rows * j >= positions) continue;
             const int pos = min(row + w.rows * j, positions - 1);
             in[j] = *(const V *)(x + pos * a.xs);
             gr[j] = *(const V *)(dy + pos * a.dys);
@@ -394,6 +423,7 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
         float s = 0.f, sx = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (w.rows * j >= positions) continue;
             __builtin_amdgcn_sched_barrier(0);
             if (MODE == CHUNK_RESULT || w.c < 0 || row + w.rows * j >= positions) continue;
 #pragma unroll
@@ -423,7 +453,11 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
         }
         const float ma = d_of[w.group] / m, mb = dx_of[w.group] / m;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) { in[j].again(); gr[j].again(); }
+        for (int j = 0; j < NV; ++j) {
+            if (w.rows * j >= positions) continue;
+            in[j].again();
+            gr[j].again();
+        }
         T *dx = (T *)a.y + start * a.ys + channel;
         if (w.c >= 0)
 #pragma unroll
@@ -590,12 +624,16 @@ struct Cut {
     int per_group, tile_groups, tiles, chunk, chunks;
     int walkers;                     // gradient: blocks that share the samples out
 };
-constexpr int TILE_VECTORS = 8, GRAD_VECTORS = 4;      // of a tensor per thread: the gradient has two tensors, and sums for each channel
+// Vectors of a tensor per thread: the gradient has two tensors, and sums for each channel.  More of them where they are only one or two
+// elements (38 samples of 123 positions, groups of 15 channels bf16: 17 us with 8, 10 with 16).
+constexpr int tile_vectors(int ve) { return ve >= 4 ? 8 : 16; }
+constexpr int GRAD_VECTORS = 4;
 constexpr int WIDEST = 1024, GRAD_WIDEST = 512;      // vectors of a group's channels that the threads of a tile's block take
-Cut cut_of(const ga3c_norm_desc *d, int samples, int positions, bool vectors, bool grad) {
+// most: elements of a vector that the tensors allow
+Cut cut_of(const ga3c_norm_desc *d, int samples, int positions, int most, bool grad) {
     Cut c{};
     const int size = d->dtype == GA3C_BF16 ? 2 : 4, wide = d->channels / d->groups;
-    c.ve = vectors && wide % (16 / size) == 0 ? 16 / size : 1;
+    c.ve = most >= 16 / size && wide % (16 / size) == 0 ? 16 / size : most >= 2 && wide % 2 == 0 ? 2 : 1;
     c.per_group = wide / c.ve;
     c.chunks = 1; c.chunk = positions; c.tiles = 1; c.tile_groups = d->groups;
     // (a lane's shares of dgamma and dbeta are two numbers for each of its channels)
@@ -621,7 +659,7 @@ Cut cut_of(const ga3c_norm_desc *d, int samples, int positions, bool vectors, bo
     c.tile_groups = k;
     c.tiles = (d->groups + k - 1) / k;
     const int all = k * c.per_group;
-    const int vectors_each = grad ? GRAD_VECTORS : TILE_VECTORS;
+    const int vectors_each = grad ? GRAD_VECTORS : tile_vectors(c.ve);
     c.threads = 256;
     if (all > 256 || positions > 256 / all * vectors_each) c.threads = widest;
     const int rows = c.threads / all * vectors_each;      // positions that a block holds
@@ -659,10 +697,10 @@ void launch_join(K kernel, const NormArgs &a, hipStream_t s) {
 template <class T, int VE, int ACT, int NT>
 void launch_tiles(const NormArgs &a, const Cut &c, hipStream_t s) {
     const dim3 block(NT), grid((unsigned)((int64_t)a.samples * c.tiles), c.chunks);
-    if (c.chunks == 1) { launch(norm_tile_kernel<T, VE, NT, TILE_VECTORS, TILE, ACT>, grid, block, 0, s, a); return; }
-    launch(norm_tile_kernel<T, VE, NT, TILE_VECTORS, CHUNK_SUMS, ACT>, grid, block, 0, s, a);
+    if (c.chunks == 1) { launch(norm_tile_kernel<T, VE, NT, tile_vectors(VE), TILE, ACT>, grid, block, 0, s, a); return; }
+    launch(norm_tile_kernel<T, VE, NT, tile_vectors(VE), CHUNK_SUMS, ACT>, grid, block, 0, s, a);
     launch_join(norm_join_kernel<false>, a, s);
-    launch(norm_tile_kernel<T, VE, NT, TILE_VECTORS, CHUNK_RESULT, ACT>, grid, block, 0, s, a);
+    launch(norm_tile_kernel<T, VE, NT, tile_vectors(VE), CHUNK_RESULT, ACT>, grid, block, 0, s, a);
 }
 template <class T, int VE, int ACT, int NT>
 void launch_tile_grad(const NormArgs &a, const Cut &c, hipStream_t s) {
@@ -696,18 +734,21 @@ void launch_act(const ga3c_norm_desc *d, const NormArgs &a, const Cut &c, bool g
     else launch_kernels<T, VE, GA3C_ACT_NONE>(a, c, grad, s);
 }
 void launch_all(const ga3c_norm_desc *d, const NormArgs &a, const Cut &c, bool grad, hipStream_t s) {
-    if (d->dtype == GA3C_BF16) c.ve == 1 ? launch_act<bf16, 1>(d, a, c, grad, s) : launch_act<bf16, 8>(d, a, c, grad, s);
-    else c.ve == 1 ? launch_act<float, 1>(d, a, c, grad, s) : launch_act<float, 4>(d, a, c, grad, s);
+    if (d->dtype == GA3C_BF16) c.ve == 1 ? launch_act<bf16, 1>(d, a, c, grad, s) : c.ve == 2 ? launch_act<bf16, 2>(d, a, c, grad, s) : launch_act<bf16, 8>(d, a, c, grad, s);
+    else c.ve == 1 ? launch_act<float, 1>(d, a, c, grad, s) : c.ve == 2 ? launch_act<float, 2>(d, a, c, grad, s) : launch_act<float, 4>(d, a, c, grad, s);
 }
 int hip_result(const char *who) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GA3C_OK : call_fail(GA3C_EHIP, "%s: %s", who, hipGetErrorString(e));
 }
-// Vectors of 16 bytes of every tensor, and of four weights.
-bool whole_vectors(const ga3c_norm_desc *d, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, const float *gamma, const float *beta) {
-    for (const void *p : tensors) if ((uintptr_t)p % 16) return false;
-    for (int64_t s : strides) if (s % (d->dtype == GA3C_BF16 ? 8 : 4)) return false;
-    return (uintptr_t)gamma % 16 == 0 && (uintptr_t)beta % 16 == 0;
+// Elements of a vector that every tensor allows: 16 bytes (and vectors of four weights), two, or one.
+int widest_vectors(const ga3c_norm_desc *d, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, const float *gamma, const float *beta) {
+    const int size = d->dtype == GA3C_BF16 ? 2 : 4;
+    uintptr_t bytes = 0;
+    for (const void *p : tensors) bytes |= (uintptr_t)p;
+    for (int64_t s : strides) bytes |= (uintptr_t)s * size;
+    if (bytes % 16 == 0 && ((uintptr_t)gamma | (uintptr_t)beta) % 16 == 0) return 16 / size;
+    return bytes % (2 * size) == 0 ? 2 : 1;
 }
 int check_cut(const ga3c_norm_desc *d, const Cut &c, int samples, const char *who) {
     if (c.chunks > 65535) return call_fail(GA3C_EINVAL, "%s: samples of too many positions", who);
@@ -726,7 +767,7 @@ using namespace ga3c;
 extern "C" size_t ga3c_group_norm_workspace(const ga3c_norm_desc *d, int n_samples, int n_positions, int grad) {
     if (check(d, n_samples, n_positions, "ga3c_group_norm_workspace") != GA3C_OK || n_samples == 0) return 0;
     size_t most = 0;
-    for (bool vectors : {false, true}) {        // whether the tensors allow them is not known here
+    for (int vectors : {1, 2, 8}) {        // what the tensors allow is not known here
         const Cut c = cut_of(d, n_samples, n_positions, vectors, grad != 0);
         most = std::max(most, sums_floats(d, c, n_samples) + (grad ? partial_floats(d, c) : 0));
     }
@@ -751,7 +792,7 @@ extern "C" int ga3c_group_norm(const ga3c_norm_desc *d, const void *x, int64_t x
     if ((uintptr_t)stats % 8) return call_fail(GA3C_EINVAL, "%s: stats not aligned to 8 bytes", who);
     if (x == y) return call_fail(GA3C_EINVAL, "%s: the result is the input", who);
     if ((rc = check_workspace(d, n_samples, n_positions, 0, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
-    const Cut c = cut_of(d, n_samples, n_positions, whole_vectors(d, {x, y}, {x_stride, y_stride}, gamma, beta), false);
+    const Cut c = cut_of(d, n_samples, n_positions, widest_vectors(d, {x, y}, {x_stride, y_stride}, gamma, beta), false);
     if ((rc = check_cut(d, c, n_samples, who)) != GA3C_OK) return rc;
     NormArgs a = args_of(d, c, n_samples, n_positions, workspace);
     a.x = x; a.xs = x_stride; a.y = y; a.ys = y_stride; a.gamma = gamma; a.beta = beta; a.stats = stats;
@@ -774,7 +815,7 @@ extern "C" int ga3c_group_norm_grad(const ga3c_norm_desc *d, const void *x, int6
         if ((uintptr_t)stats % 8) return call_fail(GA3C_EINVAL, "%s: stats not aligned to 8 bytes", who);
         if (dx == x || dx == dy) return call_fail(GA3C_EINVAL, "%s: the result is an input", who);
         if ((rc = check_workspace(d, n_samples, n_positions, 1, workspace, workspace_bytes, who)) != GA3C_OK) return rc;
-        c = cut_of(d, n_samples, n_positions, whole_vectors(d, {x, dy, dx}, {x_stride, dy_stride, dx_stride}, gamma, beta), true);
+        c = cut_of(d, n_samples, n_positions, widest_vectors(d, {x, dy, dx}, {x_stride, dy_stride, dx_stride}, gamma, beta), true);
         if ((rc = check_cut(d, c, n_samples, who)) != GA3C_OK) return rc;
     }
     NormArgs a = args_of(d, c, n_samples, n_positions, workspace);
