@@ -122,6 +122,7 @@ __device__ inline float lanes_sum(float v, int lanes) {
 
 // ------------------------------------------------------------------------ rows --
 
+// 2560 samples of 4 groups of 32 fp32: 3.4 us (2.6 MB: start and end of a launch).
 template <class T, int VE, int NV, int ACT>
 __global__ __launch_bounds__(256) void norm_rows_kernel(const NormArgs a, int lg) {
     typedef Pack<T, VE> V;
@@ -170,7 +171,8 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const NormArgs a, int lg
     if (a.stats && li == 0) *(float2 *)(a.stats + 2 * u) = float2{mean, rstd};
 }
 
-// A wavefront keeps its groups and walks over samples, so that its share of dgamma and dbeta stays in registers.
+// A wavefront keeps its groups and walks over samples, so that its share of dgamma and dbeta stays in registers.  8192 samples of 16
+// groups of 64 bf16: 15.7 us (50 MB, 3.2 TB/s), and 4.2 for dgamma and dbeta from the shares.
 template <class T, int VE, int NV, int ACT>
 __global__ __launch_bounds__(256) void norm_rows_grad_kernel(const NormArgs a, int lg) {
     typedef Pack<T, VE> V;
@@ -390,7 +392,8 @@ __global__ __launch_bounds__(NT, 8) void norm_tile_kernel(const NormArgs a) {
     }
 }
 
-// A block keeps its groups (and its chunk) and walks over samples.
+// A block keeps its groups (and its chunk) and walks over samples.  37 samples of 81 positions, 96 channels fp32: 10.5 us (3.5 MB: the
+// latency of a block's sums), and 2 for dgamma and dbeta.
 template <class T, int VE, int NT, int NV, int MODE, int ACT>
 __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
     typedef Pack<T, VE> V;
@@ -492,7 +495,8 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
 }
 
 // ------------------------------------------------------------------ wide groups --
-// Groups of more channels than a block has threads for: a block goes over one group of one sample as often as it needs to.
+// Groups of more channels than a block has threads for: a block goes over one group of one sample as often as it needs to.  Made for
+// being right at sizes that no network here has, not for speed.
 
 __device__ inline float block_sum(float v, float *sh) {
     v = lanes_sum(v, 64);
@@ -569,7 +573,7 @@ __global__ __launch_bounds__(64) void norm_wide_weights_kernel(const NormArgs a)
     a.partial[((int64_t)blockIdx.y * 2 + 1) * a.channels + c] = s;
 }
 
-// dgamma and dbeta from the shares of `rows` blocks, in a fixed order.  A block takes 64 channels, sixteen threads of each.
+// dgamma and dbeta from the shares of the blocks, in a fixed order.  A block takes 64 channels, sixteen threads of each.
 __global__ __launch_bounds__(1024) void norm_weights_kernel(const NormArgs a) {
     __shared__ float part[16][64];
     const int64_t all = 2 * (int64_t)a.channels, c = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
