@@ -77,8 +77,12 @@ CASES = [
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("case", range(len(CASES)))
 def test_attention_and_its_gradient(case, dtype):
-    lens, h, dk, dv, states, starts, decay, fused = CASES[case]
     print(f"attention case {case} {dtype}", flush=True)
+    check_attention(CASES[case], dtype)
+
+
+def check_attention(case, dtype):
+    lens, h, dk, dv, states, starts, decay, fused = case
     s = make(lens, h, dk, dv, dtype, states, starts, fused)
     n, segs, scale = sum(lens), len(lens), dk ** -0.5
     out = torch.full((n, h, dv), float("nan"), dtype=dtype, device="cuda")
@@ -106,6 +110,14 @@ def test_attention_and_its_gradient(case, dtype):
     for got, a, m, what in zip((dq, dk_, dv_), want, mags, ("dq", "dk", "dv")):
         near(got, a, m, factors, what, dtype)
     near(dstate, want[3], mags[3], factors, "dstate_in")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(62, 30), (30, 126), (114, 61), (126, 90)])
+def test_rows_of_whole_words_and_odd_ones(dk, dv, dtype):
+    """Sizes that are no multiple of 16 bytes, on tiles that are full, end early, and are cut by starts."""
+    print(f"attention {dk} {dv} {dtype}", flush=True)
+    check_attention(([64, 300, 33, 129], 2, dk, dv, True, 0.01, [0.5, 0.99], False), dtype)
 
 
 def test_gradient_against_differences():

@@ -143,6 +143,16 @@ def test_calls_that_are_too_large_are_refused():
         assert rc == -1 and b"too many samples" in lib.ga3c_last_error(), channels
 
 
+def test_scratch_is_a_state_per_span_whatever_the_segments():
+    lib = g.load_library()
+    d = desc(heads=2, key=64, value=128)
+    for tokens in (1, 127, 128, 5000, 1 << 20):
+        for segments in (1, 3, 700, 60000, 300000):
+            for grad in (0, 1):
+                most = (1 + grad) * (tokens // 128) * 2 * (64 * 128 + 1) * 4
+                assert lib.ga3c_decay_attention_workspace(C.byref(d), segments, tokens, grad) <= most, (tokens, segments)
+
+
 def test_binding_refuses_cpu_tensors():
     x = torch.zeros(4, 2, 16)
     with pytest.raises(g.Ga3cError, match="GPU tensor"):
