@@ -80,13 +80,14 @@ __device__ __forceinline__ void split3_pair(float x, float y, uint32_t &hi, uint
 }
 
 // One dword per lane from base + off (bytes) to lds + 4 * lane; base and lds are the same for the whole wavefront.  The caller
-// waits for vmcnt itself: the compiler, which would wait for every such load in front of the next LDS read, does not see it.
+// waits for vmcnt itself: the compiler, which would wait for every such load in front of the next LDS read, does not see it.  m0
+// needs a wait state between its scalar write and the load, which the compiler does not put into inline assembly.
 __device__ __forceinline__ void load_dword_to_lds(const void *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // The same with 16 bytes per lane, to lds + 16 * lane.
 __device__ __forceinline__ void load_vec_to_lds(const void *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;

@@ -343,16 +343,17 @@ __device__ inline const void *uniform(const void *p) {
     return (const void *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
 // 16 bytes per lane to lds + 16 * lane; lds is the same for the whole wavefront.  The caller waits for vmcnt itself: the compiler,
-// which would wait for every such load in front of the next LDS read, does not see it.
+// which would wait for every such load in front of the next LDS read, does not see it.  m0 needs a wait state between its scalar
+// write and the load, which the compiler does not put into inline assembly.
 __device__ inline void piece_to_lds(const void *from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
 }
 __device__ inline void piece_to_lds(const void *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 // The same with 4 bytes per lane.
 __device__ inline void word_to_lds(const void *from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
 }
 // VE elements of a row from element `i` on, zero behind its `dim` elements; rows begin anywhere.
 template <class T>
