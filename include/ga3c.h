@@ -470,8 +470,8 @@ typedef struct {
  *   workspace_dev scratch of at least ga3c_decay_attention_workspace() bytes,
  *                 16-byte aligned, contents irrelevant before and after; calls
  *                 that may overlap need one each
- * Products of fp32 tensors and all states are fp32 sums; with bfloat16 tensors
- * an output is within a few roundings to bfloat16 of the exact one.  A number
+ * All sums and states are fp32; a bfloat16 output is rounded once, after sums
+ * whose terms are off by 2^-16 at most.  A number
  * that is not finite reaches what it is part of and nothing else; an infinity
  * may arrive there as NaN. */
 int ga3c_decay_attention(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,

@@ -188,10 +188,14 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// A fragment is 16 bytes of one lane: KB numbers of the contraction in the wavefront, VE of them in the lane.
+// A fragment is 16 bytes of one lane: KB numbers of the contraction in the wavefront, VE of them in the lane.  With bfloat16 tensors what
+// is computed on the way (weighted scores, rows with their decay, the state) is fp32, and goes into a product as several bfloat16 terms:
+// a row with its decay as ROW_TERMS, all of its 24 bits, because states are fp32; a score and a state that is read out as two, which
+// miss 2^-16 of it where the result's own rounding misses 2^-8.  (With one term for rows and scores the errors were 2.3e-3 instead of
+// the result's rounding, 1.7e-3; 16384 tokens, 8 heads of 128, 80 us instead of 94.)
 template <class T> struct Tile;
 template <> struct Tile<float> {
-    static constexpr int KB = 16, VE = 4, TERMS = 1;
+    static constexpr int KB = 16, VE = 4, ROW_TERMS = 1, SCORE_TERMS = 1;
     typedef f32x4 Frag;
     typedef f32x4 Quad;
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -202,7 +206,7 @@ template <> struct Tile<float> {
     __device__ static Quad quad(f32x4 v) { return v; }
 };
 template <> struct Tile<bf16> {
-    static constexpr int KB = 32, VE = 8, TERMS = 3;
+    static constexpr int KB = 32, VE = 8, ROW_TERMS = 3, SCORE_TERMS = 2;
     typedef bf16x8 Frag;
     typedef bf16x4 Quad;
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -274,8 +278,15 @@ struct ChunkLds {
     static constexpr int C = tile_positions(sizeof(T) == 2, CP, RP, MAIN);
     static constexpr int NT = CP > 64 || RP > 64 ? 512 : 256;                // threads: sixteen rows of the state per wavefront
     static constexpr int COL = 0, ROW = COL + Image<T, C, CP>::BYTES, BY = ROW + Image<T, C, RP>::BYTES, SET = BY + (MAIN ? Image<T, C, CP>::BYTES : 0);
-    static constexpr int JB = C + W::VE;                                  // pitch of P
-    static constexpr int P = 2 * SET, PW = P + (MAIN ? C * JB * (int)sizeof(T) : 0), FW = PW + (C + 4) * 4, ODD = FW + C * 4, BYTES = ODD + 16;
+    // P: the rows of tile `it` are as long as the steps of their contraction, and VE more against bank conflicts
+    static constexpr int EACH = W::KB / 16;
+    __host__ __device__ static constexpr int p_pitch(int it) { return W::KB * (it / EACH + 1) + W::VE; }
+    __host__ __device__ static constexpr int p_tile(int it) {
+        const int steps = it / EACH;
+        return 16 * (W::KB * (EACH * steps * (steps + 1) / 2 + (it - EACH * steps) * (steps + 1)) + W::VE * it);
+    }
+    static constexpr int P_TERM = p_tile(C / 16);
+    static constexpr int P = 2 * SET, PW = P + (MAIN ? W::SCORE_TERMS * P_TERM * (int)sizeof(T) : 0), FW = PW + (C + 4) * 4, ODD = FW + C * 4, BYTES = ODD + 16;
 };
 
 // The lane's number as if it were new: places that are made of it are worked out where they are used, not kept in registers from
@@ -434,8 +445,8 @@ __device__ inline bool not_finite(uint4 v) {
 }
 
 // MAIN: outputs, and the state behind the segment.  Otherwise the state that each span but a segment's last one makes of nothing,
-// which decay_spans_kernel turns into the states between the spans.  TERMS: of a row with its decay in the state's sum.
-template <class T, int CP, int RP, bool MAIN, int TERMS>
+// which decay_spans_kernel turns into the states between the spans.
+template <class T, int CP, int RP, bool MAIN>
 __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chunk_kernel(const DecayJob job) {
     typedef Tile<T> W;
     typedef ChunkLds<T, CP, RP, MAIN> L;
@@ -559,9 +570,15 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     const float w = j <= i && j >= fresh ? pw[max(i - j, 0)] * p.col_scale : 0.f;
                     s[e] = w == 0.f ? 0.f : s[e] * w;
                 }
-                *(typename W::Quad *)(P + i * L::JB + 16 * jt + 4 * g) = W::quad(s);
-                // the fragment above the diagonal that shares a contraction step with this tile
-                if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(P + i * L::JB + 16 * (jt + 1) + 4 * g) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
+                T *const pi = P + L::p_tile(it) + l16 * L::p_pitch(it) + 16 * jt + 4 * g;
+#pragma unroll
+                for (int term = 0; term < W::SCORE_TERMS; ++term) {
+                    const typename W::Quad w = W::quad(s);
+                    *(typename W::Quad *)(pi + term * L::P_TERM) = w;
+                    if (term + 1 < W::SCORE_TERMS) s -= __builtin_convertvector(w, f32x4);
+                    // the fragment above the diagonal that shares a contraction step with this tile
+                    if (it == jt && KB > 16 && it % 2 == 0) *(typename W::Quad *)(pi + term * L::P_TERM + 16) = W::quad(f32x4{0.f, 0.f, 0.f, 0.f});
+                }
             }
             // what the state says
             if (mine) {
@@ -573,7 +590,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     if constexpr (KB == 16) {
 #pragma unroll
                         for (int it = 0; it < IT; ++it) acc[it] = W::mma(x[c], IC::along(now + L::BY, along, it, c), acc[it]);
-                    } else {       // two terms of the state, 16 bits: one alone doubles the error of the result's own rounding
+                    } else {       // two terms of the state
                         const f32x4 x0 = x[2 * c % CT], x1 = x[(2 * c + 1) % CT];
                         const bf16x4 h0 = W::quad(x0), h1 = W::quad(x1);
                         const bf16x4 l0 = W::quad(x0 - __builtin_convertvector(h0, f32x4)), l1 = W::quad(x1 - __builtin_convertvector(h1, f32x4));
@@ -614,7 +631,9 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int k = 0; k * KB <= 16 * it; ++k)
-                            acc[it] = W::mma(rowf[k], *(const typename W::Frag *)(P + (16 * it + l16) * L::JB + k * KB + g * VE), acc[it]);
+#pragma unroll
+                            for (int term = 0; term < W::SCORE_TERMS; ++term)
+                                acc[it] = W::mma(rowf[k], *(const typename W::Frag *)(P + term * L::P_TERM + L::p_tile(it) + l16 * L::p_pitch(it) + k * KB + g * VE), acc[it]);
                         const int pos = 16 * it + l16, o = 16 * wave + 4 * g;
                         const typename W::Quad w = W::quad(acc[it] * p.out_scale);
                         T *out = (T *)(out_tile + (uint32_t)(back ? n - 1 - pos : pos) * out_step);
@@ -628,18 +647,18 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     }
                 }
                 // rows with their decay, in place of the keys: a wavefront needs its own rows only
-                typename W::Frag rs[TERMS][KT];
+                typename W::Frag rs[W::ROW_TERMS][KT];
 #pragma unroll
                 for (int k = 0; k < KT; ++k) {
                     float v[VE];
 #pragma unroll
                     for (int e = 0; e < VE; ++e) v[e] = (float)rowf[k][e] * fw[KB * k + VE * g + e];
 #pragma unroll
-                    for (int term = 0; term < TERMS; ++term)
+                    for (int term = 0; term < W::ROW_TERMS; ++term)
 #pragma unroll
                         for (int e = 0; e < VE; ++e) {
                             rs[term][k][e] = from_f32<T>(v[e]);
-                            if (term + 1 < TERMS) v[e] -= (float)rs[term][k][e];
+                            if (term + 1 < W::ROW_TERMS) v[e] -= (float)rs[term][k][e];
                         }
                 }
                 const float carry = cuts ? 0.f : pw[n];
@@ -657,7 +676,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     for (int k = 0; k < KT; ++k) {
                         colf = IC::across(now + L::COL, col_across, ct, k);
 #pragma unroll
-                        for (int term = 0; term < TERMS; ++term) x[ct] = W::mma(colf, rs[term][k], x[ct]);
+                        for (int term = 0; term < W::ROW_TERMS; ++term) x[ct] = W::mma(colf, rs[term][k], x[ct]);
                     }
                 }
             }
@@ -884,10 +903,10 @@ hipError_t launch_recurrent(const DecayJob &job, int passes, int heads, hipStrea
     });
 }
 
-template <class T, int CP, int RP, bool MAIN, int TERMS>
+template <class T, int CP, int RP, bool MAIN>
 hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipStream_t s) {
     static size_t lds_set = 0;
-    const auto kernel = decay_chunk_kernel<T, CP, RP, MAIN, TERMS>;
+    const auto kernel = decay_chunk_kernel<T, CP, RP, MAIN>;
     constexpr size_t lds = ChunkLds<T, CP, RP, MAIN>::BYTES;
     if (lds > 64 * 1024 && lds_set == 0) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -897,20 +916,11 @@ hipError_t launch_chunk_kernel(const DecayJob &job, int passes, int heads, hipSt
     launch(kernel, dim3((job.items + 7) / 8 * 8, heads, passes), dim3(ChunkLds<T, CP, RP, MAIN>::NT), lds, s, job);
     return hipGetLastError();
 }
-// States are fp32 where they are handed out: a bfloat16 key with its decay then goes in as three terms, else as one.
-template <class T, int CP, int RP, bool MAIN>
-hipError_t launch_chunk_terms(const DecayJob &job, int passes, int heads, hipStream_t s) {
-    bool out = false;
-    for (int i = 0; i < passes; ++i) out = out || job.pass[i].x_out;
-    if constexpr (Tile<T>::TERMS > 1)
-        if (out) return launch_chunk_kernel<T, CP, RP, MAIN, Tile<T>::TERMS>(job, passes, heads, s);
-    return launch_chunk_kernel<T, CP, RP, MAIN, 1>(job, passes, heads, s);
-}
 template <class T, bool MAIN>
 hipError_t launch_chunk(const DecayJob &job, int passes, int heads, hipStream_t s) {
     const bool wide_rows = job.pass[0].rows > 64;
-    if (job.pass[0].cols > 64) return wide_rows ? launch_chunk_terms<T, 128, 128, MAIN>(job, passes, heads, s) : launch_chunk_terms<T, 128, 64, MAIN>(job, passes, heads, s);
-    return wide_rows ? launch_chunk_terms<T, 64, 128, MAIN>(job, passes, heads, s) : launch_chunk_terms<T, 64, 64, MAIN>(job, passes, heads, s);
+    if (job.pass[0].cols > 64) return wide_rows ? launch_chunk_kernel<T, 128, 128, MAIN>(job, passes, heads, s) : launch_chunk_kernel<T, 128, 64, MAIN>(job, passes, heads, s);
+    return wide_rows ? launch_chunk_kernel<T, 64, 128, MAIN>(job, passes, heads, s) : launch_chunk_kernel<T, 64, 64, MAIN>(job, passes, heads, s);
 }
 
 // Calls go(job, passes) for each group of passes that one launch can take: those that `together` says of.
@@ -1142,7 +1152,7 @@ extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_he
     j.pass[0] = pass_of(k, v, dout, dq, key, value, 1, 0, d->scale, 1.f, state_in, nullptr, forward);
     j.pass[1] = pass_of(q, dout, v, dk, key, value, 1, 1, 1.f, d->scale, dstate_out, nullptr, backward);
     j.pass[2] = pass_of(dout, q, k, dv, value, key, 0, 1, 1.f, d->scale, dstate_out, dstate_in, backward);
-    const int sources[] = {0, 2};         // the one that knows whether dstate_in is wanted, and its states in 32 bits
+    const int sources[] = {0, 2};         // one of each direction
     return hip_result(run(d, j, 3, sources, 2, (hipStream_t)stream), who);
 }
 
