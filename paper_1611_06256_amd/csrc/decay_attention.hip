@@ -687,7 +687,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
         set = L::SET - set;
     }
     float *x_out = !MAIN ? p.spans + place * size : last && p.x_out ? p.x_out + ((size_t)seg * heads + head) * size : nullptr;
-    if (!MAIN && tid == 0) p.spans[(size_t)(job.n_tokens / job.span) * heads * size + place] = passes ? 1.f : 0.f;
+    if (!MAIN && tid == 0) p.passes[place] = passes ? 1.f : 0.f;
     if (!x_out || !mine) return;
     const bool quads_out = !turned && cols % 4 == 0 && (uintptr_t)x_out % 16 == 0;
     const bool nothing = MAIN && back && whole > 0 && job.starts && job.starts[first];      // the first token knows of no state
@@ -720,7 +720,7 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
     if (e >= (int)size) return;
     const size_t place = (size_t)(first / job.span) * heads + head;
     float *at_span = p.spans + place * size + e;
-    const float *passes = p.spans + (size_t)(job.n_tokens / job.span) * heads * size + place;
+    const float *passes = p.passes + place;
     const float w = (float)power((double)job.decay[head], job.span);
     V x{};
     if (p.x_in) __builtin_memcpy(&x, p.x_in + ((size_t)seg * heads + head) * size + e, sizeof x);
@@ -993,7 +993,9 @@ void plan(DecayJob &job, const ga3c_decay_desc *d, bool grad) {
     job.items = job.brief >= 0 ? job.n_tokens / (job.brief + 1) + 1
                                : job.seg_start ? job.n_tokens / job.span + job.n_segments : job.n_segments * (job.len / job.span + 1);
 }
-size_t spans_floats(const DecayJob &job, int heads, size_t size) { return (size_t)(job.n_tokens / job.span) * heads * (size + 1); }
+// Scratch: the states between the spans of each direction, and behind all of them a number for each state.  (The states of a second
+// direction behind the first one's numbers would lie anywhere, and be read and written one element at a time.)
+size_t span_places(const DecayJob &job, int heads) { return (size_t)(job.n_tokens / job.span) * heads; }
 
 // passes: of outputs; sources: those of them whose spans' states are made (one forward, one backward)
 template <class T>
@@ -1078,8 +1080,8 @@ DecayJob job_of(const ga3c_decay_desc *d, const int32_t *seg_start, const uint8_
     return j;
 }
 DecayPass pass_of(const ga3c_heads *row, const ga3c_heads *col, const ga3c_heads *by, const ga3c_heads *out, int rows, int cols, int turned, int back,
-                  float out_scale, float col_scale, const float *x_in, float *x_out, float *spans) {
-    return DecayPass{view(row), view(col), view(by), view(out), rows, cols, turned, back, out_scale, col_scale, x_in, x_out, spans};
+                  float out_scale, float col_scale, const float *x_in, float *x_out, float *spans, float *passes) {
+    return DecayPass{view(row), view(col), view(by), view(out), rows, cols, turned, back, out_scale, col_scale, x_in, x_out, spans, passes};
 }
 hipError_t run(const ga3c_decay_desc *d, DecayJob &j, int passes, const int *sources, int n_sources, hipStream_t s) {
     return d->dtype == GA3C_BF16 ? run_job<bf16>(j, passes, sources, n_sources, d->n_heads, s) : run_job<float>(j, passes, sources, n_sources, d->n_heads, s);
@@ -1095,7 +1097,7 @@ extern "C" size_t ga3c_decay_attention_workspace(const ga3c_decay_desc *d, int n
     if (check_desc(d, "ga3c_decay_attention_workspace") != GA3C_OK || n_segments < 1 || n_tokens < 1) return 0;
     // the gradient has states of both directions
     const DecayJob j = job_of(d, (const int32_t *)1, nullptr, n_segments, n_tokens, grad);
-    return (grad ? 2 : 1) * sizeof(float) * spans_floats(j, d->n_heads, (size_t)d->key_dim * d->value_dim);
+    return (grad ? 2 : 1) * sizeof(float) * span_places(j, d->n_heads) * ((size_t)d->key_dim * d->value_dim + 1);
 }
 
 size_t ga3c::decay_workspace_most(const ga3c_decay_desc *d, int n_tokens) {
@@ -1121,7 +1123,8 @@ extern "C" int ga3c_decay_attention(const ga3c_decay_desc *d, const ga3c_heads *
     if (workspace_bytes < need) return call_fail(GA3C_EINVAL, "%s: workspace too small", who);
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
     DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens, false);
-    j.pass[0] = pass_of(v, k, q, out, d->value_dim, d->key_dim, 0, 0, d->scale, 1.f, state_in, state_out, (float *)workspace);
+    float *const spans = (float *)workspace, *const passes = spans + span_places(j, d->n_heads) * d->key_dim * d->value_dim;
+    j.pass[0] = pass_of(v, k, q, out, d->value_dim, d->key_dim, 0, 0, d->scale, 1.f, state_in, state_out, spans, passes);
     const int sources[] = {0};
     return hip_result(run(d, j, 1, sources, 1, (hipStream_t)stream), who);
 }
@@ -1147,11 +1150,12 @@ extern "C" int ga3c_decay_attention_grad(const ga3c_decay_desc *d, const ga3c_he
     if (need && (!workspace || (uintptr_t)workspace % 16)) return call_fail(GA3C_EINVAL, "%s: workspace null or not aligned to 16 bytes", who);
     DecayJob j = job_of(d, seg_start, starts, n_segments, n_tokens, true);
     const int key = d->key_dim, value = d->value_dim;
-    float *forward = (float *)workspace, *backward = forward + spans_floats(j, d->n_heads, (size_t)key * value);
+    const size_t places = span_places(j, d->n_heads), states = places * key * value;
+    float *const forward = (float *)workspace, *const backward = forward + states, *const passes = backward + states, *const passes_back = passes + places;
     // the states in front of the tokens once more, read out by dout; the gradient of the state behind each token, read out by v and k
-    j.pass[0] = pass_of(k, v, dout, dq, key, value, 1, 0, d->scale, 1.f, state_in, nullptr, forward);
-    j.pass[1] = pass_of(q, dout, v, dk, key, value, 1, 1, 1.f, d->scale, dstate_out, nullptr, backward);
-    j.pass[2] = pass_of(dout, q, k, dv, value, key, 0, 1, 1.f, d->scale, dstate_out, dstate_in, backward);
+    j.pass[0] = pass_of(k, v, dout, dq, key, value, 1, 0, d->scale, 1.f, state_in, nullptr, forward, passes);
+    j.pass[1] = pass_of(q, dout, v, dk, key, value, 1, 1, 1.f, d->scale, dstate_out, nullptr, backward, passes_back);
+    j.pass[2] = pass_of(dout, q, k, dv, value, key, 0, 1, 1.f, d->scale, dstate_out, dstate_in, backward, passes_back);
     const int sources[] = {0, 2};         // one of each direction
     return hip_result(run(d, j, 3, sources, 2, (hipStream_t)stream), who);
 }

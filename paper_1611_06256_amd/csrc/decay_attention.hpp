@@ -21,7 +21,8 @@ struct DecayPass {
     float out_scale, col_scale;
     const float *x_in;               // nullptr: zero
     float *x_out;                    // nullptr: not wanted
-    float *spans;                    // states between the spans of a segment, and behind them whether a span passes its own on
+    float *spans;                    // states between the spans of a segment
+    float *passes;                   // whether a span passes the state in front of it on: 1, or 0
 };
 struct DecayJob {
     DecayPass pass[3];               // one grid: a pass per z
