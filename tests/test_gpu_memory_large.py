@@ -1,5 +1,5 @@
-"""The memory operators where a call is large enough for the variants that small ones do not take: spans' states four numbers at a time,
-and a second direction's that lie behind an odd number of the first one's.
+"""The memory operators where a call is large enough for the variants that small ones do not take: states past the caches, spans' states
+four numbers at a time, and a second direction's that lie behind an odd number of the first one's.
 
 M is a result's sum of products with every factor's magnitude in its place; bounds are those of fp32 sums, (2 * tokens + dims + 24) *
 2^-24 * M, and with bfloat16 tensors 2^-8 of the result and 2^-16 * M more."""
@@ -72,3 +72,35 @@ def test_many_large_states_between_spans(segments, tokens, heads, dk, dv, dtype)
     want, size = (exact(s, decay, scale, f) for f in (lambda t: t, torch.abs))
     for what in got:
         near(got[what].view(want[what].shape), want[what], size[what], 2 * tokens + dk + dv + 24, what, F32 if "state" in what else dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,slots,heads,dk,dv", [(300, 330, 16, 64, 64), (150, 151, 8, 128, 128), (1100, 1100, 8, 20, 100)])
+def test_steps_of_states_past_the_caches(n, slots, heads, dk, dv, dtype):
+    """A slot twice and three times, padded entries, starts."""
+    print(f"steps {n} {slots} {heads} {dk} {dv} {dtype}", flush=True)
+    assert n * heads * dk * dv * 4 >= 64 << 20
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    decay, scale = [0.5 + 0.5 * i / (heads - 1) for i in range(heads)], dk ** -0.5
+    states = torch.randn(slots, heads, dv, dk, generator=gen, device="cuda")
+    q, k, v = (torch.randn(n, heads, w, generator=gen, device="cuda").to(dtype) for w in (dk, dk, dv))
+    where = torch.randperm(slots, generator=gen, device="cuda")[:n].to(torch.int32)
+    where[7], where[n // 2], where[n - 1] = -1, where[3], where[3]
+    where[20], where[n - 2] = slots, where[11]
+    starts = (torch.rand(n, generator=gen, device="cuda") < 0.1).to(torch.uint8)
+    starts[n // 2] = 0
+    kept, size = states.double(), states.double().abs()
+    out = torch.full((n, heads, dv), float("nan"), dtype=dtype, device="cuda")
+    g.decay_attention_step(q, k, v, decay, states, out, slots=where, starts=starts, scale=scale)
+    torch.cuda.synchronize()
+    d = torch.tensor(decay, dtype=F32).double().cuda()[:, None, None]
+    want, mag = (torch.empty(n, heads, dv, dtype=torch.float64, device="cuda") for _ in range(2))
+    for i, (at, new) in enumerate(zip(where.tolist(), starts.tolist())):
+        for x, to, f in ((kept, want, lambda t: t), (size, mag, torch.abs)):
+            a, b, c = (f(t[i].double()) for t in (q, k, v))
+            st = (x[at] * d if 0 <= at < slots and not new else 0) + c[:, :, None] * b[:, None, :]
+            to[i] = scale * (st * a[:, None, :]).sum(-1)
+            if 0 <= at < slots:
+                x[at] = st
+    near(out, want, mag, 2 * 3 + dk + 24, "out", dtype)
+    near(states, kept, size, 2 * 3 + 24, "states")
