@@ -471,9 +471,10 @@ typedef struct {
  *                 16-byte aligned, contents irrelevant before and after; calls
  *                 that may overlap need one each
  * All sums and states are fp32; a bfloat16 output is rounded once, after sums
- * whose terms are off by 2^-16 at most.  A number
- * that is not finite reaches what it is part of and nothing else; an infinity
- * may arrive there as NaN. */
+ * whose terms are off by 2^-16 at most.  A number that is not finite reaches
+ * what it is part of and nothing else; an infinity may arrive there as NaN.
+ * (Of a state with decay 0 nothing is part of what comes, of one with any other
+ * decay all is, however small its share.) */
 int ga3c_decay_attention(const ga3c_decay_desc *desc, const ga3c_heads *q, const ga3c_heads *k, const ga3c_heads *v,
                          const ga3c_heads *out, const int32_t *seg_start_dev, const uint8_t *starts_dev, int n_segments,
                          int n_tokens, const float *state_in_dev, float *state_out_dev, void *workspace_dev,

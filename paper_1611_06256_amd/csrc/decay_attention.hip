@@ -296,10 +296,10 @@ __device__ inline int fresh_lane() {
     asm volatile("" : "+v"(lane));
     return lane;
 }
-// Nothing is left of what is multiplied with zero, whatever it was.
-__device__ inline f32x4 scaled(f32x4 v, float w) {
+// Nothing is left of what is not kept, whatever it was.
+__device__ inline f32x4 scaled(f32x4 v, float w, bool kept) {
     const f32x4 r = v * w;
-    return f32x4{w == 0.f ? 0.f : r[0], w == 0.f ? 0.f : r[1], w == 0.f ? 0.f : r[2], w == 0.f ? 0.f : r[3]};
+    return f32x4{kept ? r[0] : 0.f, kept ? r[1] : 0.f, kept ? r[2] : 0.f, kept ? r[3] : 0.f};
 }
 __device__ inline double power(double d, int e) {
     double r = 1.0;
@@ -474,7 +474,9 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
     const bool back = p.back, turned = p.turned, last = to == whole;
     const int rows = p.rows, cols = p.cols, a = back ? 0 : 1;
     const float d = job.decay[head];
-    const bool fades = (float)power((double)d, C) == 0.f;           // some factors of a tile are zero
+    // With a decay of zero a token sees its own only, as if each began an episode.  (A power of another decay that is too small to be
+    // a number is a factor of zero, which takes finite numbers away and leaves the others.)
+    const bool none = d == 0.f;
     const bool pieces = whole_pieces<T>(p.col, cols) && whole_pieces<T>(p.row, rows) && whole_pieces<T>(p.by, cols);
     const uint32_t col_off = tile_offset<T, C, CP, NT>(p.col, back, tid), row_off = tile_offset<T, C, RP, NT>(p.row, back, tid),
                    by_off = MAIN ? tile_offset<T, C, CP, NT>(p.by, back, tid) : 0;
@@ -530,7 +532,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
         const int n = single ? 1 : min(C, to - base);
         const uint64_t cuts = job.starts ? __ballot(lane < n && flag && !(back && base + lane == 0)) : 0;
         const int cut = cuts ? 63 - __clzll(cuts) : -1;             // the tile's last start
-        const bool whole_tile = cuts == 0 && !fades;                // every position sees the state, and it stays
+        const bool whole_tile = cuts == 0 && !none;                // every position sees the state, and it stays
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const char *const now = lds + set;
@@ -546,7 +548,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                 rowf[k] = IR::across(now + L::ROW, row_across, wave, k);
                 wrong = wrong || not_finite<T>(__builtin_bit_cast(uint4, rowf[k]));
             }
-        if (cuts)
+        if (!whole_tile)
             for (int s = tid; s < IC::BYTES / 16; s += NT) wrong = wrong || not_finite<T>(*(const uint4 *)(now + L::COL + 16 * s));
         if (wrong && !single) *odd = 1;
         f32x4 acc[IT];
@@ -567,8 +569,8 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = 16 * jt + 4 * g + e;
-                    const float w = j <= i && j >= fresh ? pw[max(i - j, 0)] * p.col_scale : 0.f;
-                    s[e] = w == 0.f ? 0.f : s[e] * w;
+                    const float w = pw[max(i - j, 0)] * p.col_scale;
+                    s[e] = j <= i && j >= fresh && (j == i || !none) ? s[e] * w : 0.f;
                 }
                 T *const pi = P + L::p_tile(it) + l16 * L::p_pitch(it) + 16 * jt + 4 * g;
 #pragma unroll
@@ -608,7 +610,7 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                     const int i = 16 * it + l16;
                     const float w = pw[min(i + a, C)];
                     if (whole_tile) acc[it] = acc[it] * w;
-                    else acc[it] = scaled(acc[it], cuts & (~0ull >> (63 - i)) ? 0.f : w);
+                    else acc[it] = scaled(acc[it], w, !(cuts & (~0ull >> (63 - i))) && (i + a == 0 || !none));
                 }
             }
         }
@@ -661,14 +663,15 @@ __global__ __launch_bounds__((ChunkLds<T, CP, RP, MAIN>::NT), 2) void decay_chun
                             if (term + 1 < W::ROW_TERMS) v[e] -= (float)rs[term][k][e];
                         }
                 }
-                const float carry = cuts ? 0.f : pw[n];
+                const float carry = pw[n];
                 if (whole_tile) {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) x[ct] = x[ct] * carry;
                 } else {
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) x[ct] = scaled(x[ct], carry);
+                    for (int ct = 0; ct < CT; ++ct) x[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
+                if (!(none && back))                                // nothing of a tile stays then
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     if (ct % (MAIN ? 4 : 2) == 0) __builtin_amdgcn_sched_barrier(0);
@@ -722,6 +725,7 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
     float *at_span = p.spans + place * size + e;
     const float *passes = p.passes + place;
     const float w = (float)power((double)job.decay[head], job.span);
+    const bool none = job.decay[head] == 0.f;
     V x{};
     if (p.x_in) __builtin_memcpy(&x, p.x_in + ((size_t)seg * heads + head) * size + e, sizeof x);
     constexpr int AHEAD = 8;                              // spans whose numbers are under way together
@@ -737,7 +741,7 @@ __global__ __launch_bounds__(256) void decay_spans_kernel(const DecayJob job, in
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
             if (i + k + 1 < spans) {
-                if (f[k] == 0.f || w == 0.f) x = V{};     // whatever was in it
+                if (f[k] == 0.f || none) x = V{};         // whatever was in it
                 x = w * x + v[k];
                 *(V *)(at_span + (size_t)(i + k) * heads * size) = x;
             }
