@@ -2683,7 +2683,7 @@ static int create(const ga3c_net_desc *d, const ga3c_memory_desc *memory, int ma
     if (rc == GA3C_OK && c->nconv >= 2 && spec_matches<SpecS1>(c->geom[0], true) && spec_matches<SpecS2>(c->geom[1], false) &&
         c->off[0] % 4 == 0 && c->off[2] % 4 == 0) {
         c->cfrag_dgrad = true;
-        c->small_frames = small_launch_frames(c);
+        c->small_frames = memory ? 0 : small_launch_frames(c);      // a memory lies between what that launch does
         for (int i = 0; i < 2 && rc == GA3C_OK; ++i) {
             guard(dmalloc((void **)&c->cfrag[i], sizeof(u32x4) * CFRAG_VECS));
             if (rc == GA3C_OK && !c->rb && max_predict_batch > c->small_frames) guard(dmalloc((void **)&c->hfrag[i], sizeof(u32x4) * Conv12F16::VECS));
