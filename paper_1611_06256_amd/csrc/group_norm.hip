@@ -669,7 +669,7 @@ Cut cut_of(const ga3c_norm_desc *d, int samples, int positions, int most, bool g
     const int rows = c.threads / all * vectors_each;      // positions that a block holds
     c.chunk = std::min(positions, std::max(rows, 1));
     c.chunks = (positions + c.chunk - 1) / c.chunk;
-    c.walkers = std::max(1, std::min(samples, 2048 / (c.tiles * c.chunks)));
+    c.walkers = (int)std::max<int64_t>(1, std::min<int64_t>(samples, 2048 / ((int64_t)c.tiles * c.chunks)));
     return c;
 }
 size_t sums_floats(const ga3c_norm_desc *d, const Cut &c, int samples) { return c.chunks > 1 ? 2 * (size_t)samples * c.chunks * d->groups : 0; }
