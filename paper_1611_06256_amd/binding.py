@@ -730,7 +730,7 @@ def _decay_desc(q, v, decay, scale: float) -> _DecayDesc:
             raise Ga3cError(f"{what}: expected [tokens, heads, dim], got {tuple(t.shape)}")
     if len(decay) != q.shape[1]:
         raise Ga3cError(f"decay: expected one for each of {q.shape[1]} heads, got {len(decay)}")
-    return _decay_desc_of(q.shape[1], q.shape[2], v.shape[2], dtype, tuple(decay), scale)
+    return _decay_desc_of(q.shape[1], q.shape[2], v.shape[2], dtype, tuple(map(float, decay)), float(scale))      # numbers, not what holds them
 
 
 def _segments(n: int, seg_start, segments, starts, device):
@@ -856,7 +856,7 @@ def _norm_desc(x, groups: int, act: str, eps: float):
     positions = 1
     for size in shape[1:-1]:
         positions *= size
-    return _norm_desc_of(shape[-1], groups, dtype, _ACT[act], eps), shape[0], positions
+    return _norm_desc_of(shape[-1], groups, dtype, _ACT[act], float(eps)), shape[0], positions
 
 
 def group_norm(x, gamma, beta, groups: int, y, stats=None, act: str = "none", eps: float = 1e-5, stream=None) -> None:
