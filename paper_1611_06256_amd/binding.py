@@ -383,6 +383,11 @@ class Ga3c:
             raise Ga3cError("memory_states: the network has no memory")
         return torch.zeros(n, m.heads, m.value_dim, m.key_dim, device="cuda")
 
+    def _frames(self, frames, lead: int, what: str) -> None:
+        d = self.desc
+        if frames.dim() != lead + 3 or tuple(frames.shape[lead:]) != (d.in_c, d.in_h, d.in_w):
+            raise Ga3cError(f"{what}: expected frames of {(d.in_c, d.in_h, d.in_w)} behind {lead} dimension{'s' * (lead > 1)}, got {tuple(frames.shape)}")
+
     def _states(self, states, n: int, what: str):
         import torch
         m = self.memory
@@ -398,10 +403,15 @@ class Ga3c:
         in place; agents i32 [B], the state of each frame, or None (frame i has state i); starts u8 [B] or None, non-zero where an
         episode begins.  Output tensors that are passed in are filled."""
         import torch
+        self._frames(frames, 1, "predict_memory")
         B, n = int(frames.shape[0]), int(states.shape[0])
         for t, what in ((agents, "agents"), (starts, "starts")):
             if t is not None and t.numel() != B:
                 raise Ga3cError(f"{what}: expected {B} entries")
+        for t, each, what in ((uniforms, 1, "uniforms"), (logits, self.n_actions, "logits"), (values, 1, "values"), (probs, self.n_actions, "probs"),
+                              (actions, 1, "actions")):
+            if t is not None and t.numel() < B * each:
+                raise Ga3cError(f"{what}: {t.numel()} entries, {B * each} needed")
         _check(self._lib.ga3c_predict_memory(self._ctx, _ptr(frames, torch.uint8, "frames"), B, _ptr(agents, torch.int32, "agents"),
                                              _ptr(starts, torch.uint8, "starts"), self._states(states, n, "predict_memory"), n,
                                              _ptr(uniforms, torch.float32, "uniforms"),
@@ -415,6 +425,7 @@ class Ga3c:
         frames u8 [F,C,H,W] and the rest as for train_step_ragged.  states f32 [N, heads, value_dim, key_dim], the state of each
         segment's agent before its first frame, or None (zero); they are not changed."""
         import torch
+        self._frames(frames, 2 if seg_start is None else 1, "train_step_memory")
         if seg_start is None:
             N, F = int(frames.shape[0]), int(frames.shape[0]) * int(frames.shape[1])
         else:
