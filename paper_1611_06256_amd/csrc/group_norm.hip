@@ -50,14 +50,15 @@ __device__ inline float activation(float z) {
     if (ACT == GA3C_ACT_SILU) return z * sigmoid(z);
     return z;
 }
+// dz of dy: nothing of what arrives where the rectifier is closed, whatever it is.
 template <int ACT>
-__device__ inline float activation_slope(float z) {
-    if (ACT == GA3C_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+__device__ inline float activation_grad(float dy, float z) {
+    if (ACT == GA3C_ACT_RELU) return z > 0.f ? dy : 0.f;
     if (ACT == GA3C_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * (1.f + z * (1.f - s));
+        return dy * (s * (1.f + z * (1.f - s)));
     }
-    return 1.f;
+    return dy;
 }
 
 // VE neighbouring elements as they lie in memory: 16 bytes, two, or a single one.  again(): what was made of them so far is not kept in
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256) void norm_rows_grad_kernel(const NormArgs a, i
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 xh[j][e] = (in[j][e] - st.x) * st.y;
-                const float dz = gr[j][e] * activation_slope<ACT>(xh[j][e] * g[j][e] + b[j][e]);
+                const float dz = activation_grad<ACT>(gr[j][e], xh[j][e] * g[j][e] + b[j][e]);
                 dg[j][e] += dz * xh[j][e];
                 db[j][e] += dz;
                 d[j][e] = dz * g[j][e];
@@ -431,7 +432,7 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
             if (MODE == CHUNK_RESULT || w.c < 0 || row + w.rows * j >= positions) continue;
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float xh = (in[j][e] - st.x) * st.y, dz = gr[j][e] * activation_slope<ACT>(xh * g[e] + b[e]), d = dz * g[e];
+                const float xh = (in[j][e] - st.x) * st.y, dz = activation_grad<ACT>(gr[j][e], xh * g[e] + b[e]), d = dz * g[e];
                 dg[e] += dz * xh;
                 db[e] += dz;
                 s += d;
@@ -470,7 +471,7 @@ __global__ __launch_bounds__(NT) void norm_tile_grad_kernel(const NormArgs a) {
                 float r[VE];
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    const float xh = (in[j][e] - st.x) * st.y, dz = gr[j][e] * activation_slope<ACT>(xh * g[e] + b[e]);
+                    const float xh = (in[j][e] - st.x) * st.y, dz = activation_grad<ACT>(gr[j][e], xh * g[e] + b[e]);
                     r[e] = st.y * (dz * g[e] - ma - xh * mb);
                 }
                 *(V *)(dx + (row + w.rows * j) * a.ys) = V::of(r);
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(const NormArgs a) {
         const int64_t p = e / a.wide;
         const int c = (int)(e % a.wide);
         const float xh = (to_f32(x[p * a.xs + c]) - st.x) * st.y, g = a.gamma[c0 + c];
-        const float d = to_f32(dy[p * a.dys + c]) * activation_slope<ACT>(xh * g + a.beta[c0 + c]) * g;
+        const float d = activation_grad<ACT>(to_f32(dy[p * a.dys + c]), xh * g + a.beta[c0 + c]) * g;
         s += d; sx += d * xh;
     }
     const float ma = block_sum(s, sh) / (float)m, mb = block_sum(sx, sh) / (float)m;
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(const NormArgs a) {
         const int64_t p = e / a.wide;
         const int c = (int)(e % a.wide);
         const float xh = (to_f32(x[p * a.xs + c]) - st.x) * st.y, g = a.gamma[c0 + c];
-        const float d = to_f32(dy[p * a.dys + c]) * activation_slope<ACT>(xh * g + a.beta[c0 + c]) * g;
+        const float d = activation_grad<ACT>(to_f32(dy[p * a.dys + c]), xh * g + a.beta[c0 + c]) * g;
         dx[p * a.ys + c] = from_f32<T>(st.y * (d - ma - xh * mb));
     }
 }
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(64) void norm_wide_weights_kernel(const NormArgs a)
     for (int64_t e = each * blockIdx.y; e < last; ++e) {
         const float2 st = *(const float2 *)(a.stats + 2 * (e / a.positions * a.groups + c / a.wide));
         const float xh = (to_f32(((const T *)a.x)[e * a.xs + c]) - st.x) * st.y;
-        const float d = to_f32(((const T *)a.dy)[e * a.dys + c]) * activation_slope<ACT>(xh * a.gamma[c] + a.beta[c]);
+        const float d = activation_grad<ACT>(to_f32(((const T *)a.dy)[e * a.dys + c]), xh * a.gamma[c] + a.beta[c]);
         s += d; sx += d * xh;
     }
     a.partial[(int64_t)blockIdx.y * 2 * a.channels + c] = sx;
