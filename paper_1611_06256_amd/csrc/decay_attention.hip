@@ -180,9 +180,10 @@ __global__ __launch_bounds__(256) void decay_recurrent_kernel(const DecayJob job
 // row per lane) is that of the left operand of X by_i, so it never passes through LDS; a wavefront has sixteen of its rows.
 // The tiles go straight from memory to LDS, the next one while this one is worked on; contractions over positions read them
 // across their rows (an instruction of its own for 16 bits, single numbers for 32).
-// 16384 tokens bf16, 8 heads of 128, in 32 spans: states of the spans 27 us, states between them 11, outputs 45 (151 MB, 3.4 TB/s:
-// memory, and the beginning of a block, about 9 us).  Gradient of 4096 tokens fp32, 4 heads of 128, in 16 spans: 31, 7 and 61 (the
-// fp32 instruction, on 192 of 256 compute units: 3.6 GFLOP there, 60 TFLOP/s; 16 spans more would cost what they bring).
+// 16384 tokens bf16, 8 heads of 128, in 32 spans: states of the spans 37 us, states between them 10, outputs 55 (151 MB, 2.7 TB/s; half of
+// a wavefront's life is waiting, the matrix units are busy a sixth of the time).  Gradient of 4096 tokens fp32, 4 heads of 128, in 16
+// spans: 32, 6 and 59 (the fp32 instruction, on 192 of 256 compute units: 3.6 GFLOP there, 61 TFLOP/s; 16 spans more would cost what
+// they bring).
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -192,7 +193,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // is computed on the way (weighted scores, rows with their decay, the state) is fp32, and goes into a product as several bfloat16 terms:
 // a row with its decay as ROW_TERMS, all of its 24 bits, because states are fp32; a score and a state that is read out as two, which
 // miss 2^-16 of it where the result's own rounding misses 2^-8.  (With one term for rows and scores the errors were 2.3e-3 instead of
-// the result's rounding, 1.7e-3; 16384 tokens, 8 heads of 128, 80 us instead of 94.)
+// the result's rounding, 1.7e-3; 16384 tokens, 8 heads of 128, took 80 us a call, with these 94.)
 template <class T> struct Tile;
 template <> struct Tile<float> {
     static constexpr int KB = 16, VE = 4, ROW_TERMS = 1, SCORE_TERMS = 1;
@@ -267,8 +268,8 @@ struct Image {
 };
 
 // Positions of a tile, C.  With 16 bits the tile's fixed work asks for 64; where both sizes are 64 or less, outputs take 32, with
-// which four blocks have room on a compute unit instead of two (gradient of 16 segments of 512 tokens, 8 heads of 64: 54 us with 64,
-// 46 with 32; 16384 tokens of 8 heads of 128: 73 and 87).  With 32 bits 64 would not fit, and 16 is hardly ever faster (16 segments
+// which four blocks have room on a compute unit instead of two (us a call, gradient of 16 segments of 512 tokens, 8 heads of 64: 63 with
+// 64, 53 with 32; 16384 tokens of 8 heads of 128: 99 and 113).  With 32 bits 64 would not fit, and 16 is hardly ever faster (16 segments
 // of 1000 tokens, 8 heads of 128: 235 us with 32, 271 with 16; 32 such segments, heads of 64: 146 and 142).
 constexpr int tile_positions(bool bf, int cols, int rows, bool main) { return bf && !(main && cols <= 64 && rows <= 64) ? 64 : 32; }
 
@@ -310,7 +311,7 @@ __device__ inline double power(double d, int e) {
 
 // The item that a block takes: eight neighbours change places, by one more in the next eight and in the next head.  Blocks go to the
 // eight dies in turn, and places without a span (one behind each segment that is whole spans long) would fall to some of them only
-// (gradient of 64 segments of 512 tokens in spans of 512, 8 heads of 64 and 128 bf16: 394 us without this, 265 with).
+// (gradient of 64 segments of 512 tokens in spans of 512, 8 heads of 64 and 128 bf16: 464 us a call without this, 313 with).
 __device__ inline int item_of(int i, int head) { return (i & ~7) | ((i + (i >> 3) + head) & 7); }
 
 // (The state that span k of a segment makes of nothing, if it is not its last one, has place first token / span + k.  That is less than
@@ -399,7 +400,7 @@ __device__ inline void stage(const DecayView &v, int dim, bool whole, uint32_t o
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)to + wave * 1024);
     const bool full = whole && n == C && dim == D;
     // rows of whole words (any of 32 bits) come word by word, on their way like the pieces (gradient of 16 segments, 8190 tokens, 8 heads
-    // of 62 bf16: 131 us if they pass registers, 112; 8 heads of 64: 57)
+    // of 62 bf16: 148 us a call if they pass registers, 115; 8 heads of 64: 62)
     if (!whole && (sizeof(T) == 4 || ((uintptr_t)v.data % 4 == 0 && ((v.token | v.head | dim) % 2) == 0))) {
         constexpr int WORDS = 4 * ALL, EACH = 4 / (int)sizeof(T);
         static_assert(WORDS % NT == 0, "whole blocks of words");
@@ -947,17 +948,17 @@ hipError_t by_sizes(const DecayJob &job, int passes, Together together, F go) {
 bool recurrent_together(const DecayPass &a, const DecayPass &b) {
     return (a.rows == b.rows && a.cols == b.cols) || std::max({a.rows, a.cols, b.rows, b.cols}) <= 32;
 }
-// Chunked: passes of one kernel (gradient of 64 segments of 256 tokens bf16, 4 heads of 64 and 32: 58 us apart, 37 together).
+// Chunked: passes of one kernel (gradient of 64 segments of 256 tokens bf16, 4 heads of 64 and 32: 77 us a call apart, 35 together).
 bool chunk_together(const DecayPass &a, const DecayPass &b) { return (a.rows > 64) == (b.rows > 64) && (a.cols > 64) == (b.cols > 64); }
 
 // Tokens of a segment that a block of the chunked kernels takes: a power of two of SHORTEST_SPAN, the one that takes least time by this
 // count.  A block's time is its tiles and three more for its beginning; blocks take turns on as many places as the compute units have.
 // Two more kernels, two tiles' time, are launched unless no segment can be longer than the span; if the longest segment (by guess,
-// twice the average) is longer, they take half of the time of the outputs and as long again for what lies between.  Over 250 calls of
-// 1 to 100 segments, equal, uneven and cut at random, of 200 to 64000 tokens this is 7% behind the best of 128 to 1024 each time, 77%
-// at most (random cuts, whose longest segment is longer than guessed); us of all kernels with 128 / 256 / 512 / 1024: 16384 tokens
-// bf16, 8 heads of 128: 124 / 96 / 85 / 118 (512 taken); gradient of 4096 tokens fp32, 4 heads of 128: 103 / 99 / 170 / 318 (256);
-// gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 442 / 338 / 267 / 263 (1024).
+// twice the average) is longer, they take half of the time of the outputs and as long again for what lies between.  Over 120 calls of
+// 1 to 100 segments, equal, uneven and cut at random, of 200 to 64000 tokens this is 4% behind the best of 128 to 1024 each time, 99%
+// at most (random cuts, whose longest segment is longer than guessed; profiles/memory_operators_span_choice.txt); us a call with 128 /
+// 256 / 512 / 1024 tokens: 16384 tokens bf16, 8 heads of 128: 129 / 105 / 98 / 144 (512 taken); gradient of 4096 tokens fp32, 4 heads of
+// 128: 93 / 96 / 168 / 316 (256); gradient of 64 segments of 512 tokens bf16, 8 heads of 64 and 128: 496 / 396 / 313 / 308 (none split: 228).
 constexpr int SHORTEST_SPAN = 128;
 int span_of(int heads, int n_segments, int n_tokens, int key, int value, int passes, bool bf) {
     const bool small = key <= 64 && value <= 64;
@@ -978,11 +979,12 @@ int span_of(int heads, int n_segments, int n_tokens, int key, int value, int pas
     return best;
 }
 // The average length up to which segments take the token-by-token kernel (those of up to twice that, the rest are chunked).  What that
-// kernel does for a token grows with the state, the chunked one has its fixed work per segment, which takes longer with 32 bits.  us
-// token by token / chunked, 128 and 768 segments of 4 heads: fp32 16 and 32, 15 tokens 20 / 22 and 28 / 60; 32 and 32, 10 tokens
-// 21 / 23 and 28 / 58; 64 and 64, 7 tokens 19 / 22 and 54 / 62, 10 tokens 24 / 22 and 73 / 63; bf16 16 and 16, 10 tokens 18 / 20 and
-// 21 / 30; 32 and 32, 4.5 tokens 19 / 19 and 22 / 31, 10 tokens 29 / 20 and 34 / 31; 64 and 64, 2 tokens 12 / 20 and 35 / 33, 4.5
-// tokens 20 / 20 and 51 / 34.
+// kernel does for a token grows with the state, the chunked one has its fixed work per segment, which takes longer with 32 bits.  us a
+// call, token by token (with the launch that finds no long segment) / chunked, 768 segments of 4 heads, states in and out: fp32 16 and 32,
+// 15 tokens 20 / 40; 32 and 32, 10 tokens 24 / 40; 64 and 64, 4 tokens 53 / 49, 7 tokens 60 / 50 (without states 31 / 39 and 39 / 39);
+// 128 and 128, 5 tokens 175 / 174 (91 / 117); bf16 16 and 16, 10 tokens 17 / 22; 32 and 32, 4.5 tokens 22 / 25, 10 tokens 30 / 24; 64 and
+// 64, 2 tokens 57 / 33 (33 / 22); 128 and 128, 1 token 136 / 162 (46 / 107), 3 tokens 180 / 163 (85 / 108).  (bf16 states of
+// 64 and 64 would be faster chunked from one token on.)  128 segments take 12 to 16 us either way, the host's time and one launch more or less.
 int brief_average(int key, int value, bool bf) {
     const int size = key * value;
     if (bf) return size <= 256 ? 12 : size <= 1024 ? 5 : 3;

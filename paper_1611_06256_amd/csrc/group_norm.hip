@@ -41,7 +41,8 @@ struct NormArgs {
 };
 
 // 1 / (1 + exp(-z)) from the hardware's power of two and reciprocal, each within a unit in the last place; the exponent's rounding
-// moves the result by less than |z| 2^-24 of itself, at most 3 units where it counts.  (With the library's exponential and a full
+// moves the result by less than |z| 2^-24 of itself, at most 3 units where it counts; below z = -87 it is 0 in place of numbers
+// under 1e-37.  (With the library's exponential and a full
 // division the arithmetic of 64 maps of bfloat16 took longer than their way from and to memory.)
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 template <int ACT>
